@@ -171,8 +171,8 @@ def _run_route(s):
         ids, weights, logp = P.einet_route(s["scores"], s["coef"], s["top"], renormalise=s["renormalise"])
         if not s["train"]:
             return ids, weights, logp
-        dscores, dcoef = P.einet_route_backward(s["scores"], s["coef"], ids, weights, logp, dweights=s["dweights"],
-                                                dlogp=s["dlogp"], renormalise=s["renormalise"])
+        dscores, dcoef = P.einet_route_backward(s["scores"], s["coef"], ids, weights, s["dweights"], s["dlogp"],
+                                                renormalise=s["renormalise"])
         return ids, weights, logp, dscores, dcoef
     # sums of score and coefficient and their differences in 64 bits: neighbours are close to each other and large
     t = s["scores"].t().double()
