@@ -313,6 +313,125 @@ int einet_sample(einet_t* h, int B, const float* x_dev, const uint8_t* mask_dev,
 int einet_mixture_logp(const float* logp_dev, const float* log_coef_dev, int n_components, int B, float* out_dev,
                        void* stream);
 
+/* ---- Routing samples to the components of a mixture, and choices from logits.
+ * None of these calls needs a handle; all are asynchronous on `stream`, allocate nothing, use no floating-point atomics
+ * (results are bit-reproducible) and may be captured into a HIP graph.  The workspace of a call is in use until the
+ * call's work on the stream is done and holds nothing from one call to the next: calls that may overlap in time (on
+ * several streams, or in graphs that are replayed side by side) need workspaces of their own.  Element types: */
+enum { EINET_FLOAT32 = 0, EINET_BFLOAT16 = 1, EINET_FLOAT16 = 2 };
+#define EINET_ROUTE_MAX_COMPONENTS 1024
+#define EINET_ROUTE_MAX_TOP 16
+
+/* The `top` most probable components of every sample.  With t[c] = score[c] + log_coef[c] (formed in float64):
+ *   logp = log sum_c exp(t[c]),  p[c] = exp(t[c] - logp);
+ *   id[0..top-1]: the components with the largest t, the largest first, of equal ones the lowest first;
+ *   weight[s] = p[id[s]], or with `renormalise` p[id[s]] / sum_s p[id[s]].
+ * A component whose t is -inf or NaN is left out (p = 0); where fewer than `top` are left the other id are -1 and their
+ * weights 0, and a sample without any has logp = -inf.  Components at +inf share the whole weight.
+ *   score_dev     device, entry (c, i) of component c and sample i at c * component_stride + i * sample_stride
+ *                 elements of `dtype`: [n_components][n] as einet_mixture_logp takes it has strides (n, 1), a router's
+ *                 logits [n][n_components] have strides (1, n_components)
+ *   log_coef_dev  device, [n_components] float32, or NULL for none
+ *   id_dev        device, [n][top] int32, written;  weight_dev  device, [n][top] float32, written
+ *   logp_dev      device, [n] float32, written
+ * n = 0 is no error and does nothing.  Errors: EINET_ERR_INVALID_ARG (unknown dtype; n_components outside
+ * 1..EINET_ROUTE_MAX_COMPONENTS; top outside 1..min(n_components, EINET_ROUTE_MAX_TOP); n < 0 or n * top above 2^31 - 1;
+ * negative strides; NULL or misaligned pointers), EINET_ERR_HIP; the reason is read with einet_last_error(NULL). */
+int einet_route(const void* score_dev, int dtype, int64_t component_stride, int64_t sample_stride,
+                const float* log_coef_dev, int n_components, int64_t n, int top, int renormalise, int32_t* id_dev,
+                float* weight_dev, float* logp_dev, void* stream);
+
+/* Bytes of device workspace that einet_route_backward needs for dlog_coef_dev.  bytes: host. */
+int einet_route_workspace(int n_components, int64_t n, size_t* bytes);
+
+/* Gradient of einet_route: from dweight = dL/dweight and dlogp = dL/dlogp the gradients of the scores and of the log
+ * coefficients (which of the components were selected is taken as given).  With dweight_dev NULL and dlogp = 1 it is the
+ * E-step of the mixture: dscore[c][i] the posterior of component c, dlog_coef[c] its expected number of samples.
+ *   score_dev .. renormalise, id_dev, weight_dev: as given to and written by einet_route
+ *   dweight_dev    device, [n][top] float32, or NULL (id_dev and weight_dev may then be NULL too)
+ *   dlogp_dev      device, [n] float32, or NULL
+ *   dscore_dev     device, written completely, of `dtype`, entry (c, i) at c * dcomponent_stride + i * dsample_stride
+ *   dlog_coef_dev  device, [n_components] float32, written, or NULL; needs the workspace (einet_route_workspace bytes,
+ *                  16-byte aligned)
+ * The entries of dscore_dev must not share memory.  n = 0 writes zeros to dlog_coef_dev.  Errors as einet_route. */
+int einet_route_backward(const void* score_dev, int dtype, int64_t component_stride, int64_t sample_stride,
+                         const float* log_coef_dev, int n_components, int64_t n, int top, int renormalise,
+                         const int32_t* id_dev, const float* weight_dev, const float* dweight_dev, const float* dlogp_dev,
+                         void* dscore_dev, int64_t dcomponent_stride, int64_t dsample_stride, float* dlog_coef_dev,
+                         void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace that einet_sort needs (0 is possible).  bytes: host. */
+int einet_sort_workspace(int64_t n_slots, int n_components, size_t* bytes);
+
+/* Stable sort of slots by component.
+ *   id_dev     device, [n_slots] int32: the component of every slot; a value outside 0..n_components-1 (einet_route
+ *              writes -1) is a slot that goes nowhere
+ *   first_dev  device, [n_components + 1] int32, written: the slots of component c have the positions
+ *              first[c] .. first[c+1]-1, in the order of the slots; first[n_components] is their number
+ *   place_dev  device, [n_slots] int32, written: the position of every slot, -1 for one that goes nowhere
+ *   workspace_dev  device, einet_sort_workspace bytes, 16-byte aligned (NULL if that is 0)
+ * n_slots = 0 writes zeros to first_dev.  Errors: EINET_ERR_INVALID_ARG (n_components outside
+ * 1..EINET_ROUTE_MAX_COMPONENTS, n_slots outside 0..2^31-1, pointers, workspace), EINET_ERR_HIP. */
+int einet_sort(const int32_t* id_dev, int64_t n_slots, int n_components, int32_t* first_dev, int32_t* place_dev,
+               void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* Rows to their components: out[place[i][s]] = row[i] for the `top` slots s of each of n rows.  Rows of any elements:
+ * widths and strides are in bytes.  Positions outside 0..out_rows-1 go nowhere; rows of out_dev that no slot has are left as
+ * they were.  Different slots must have different positions, as einet_sort gives them; out_dev must not overlap row_dev.
+ *   row_dev    device, row i at i * row_stride_bytes (0: the same row for all);  place_dev  device, [n][top] int32
+ *   out_dev    device, row p at p * out_stride_bytes
+ * The gradient of row is einet_combine of the gradient of out without weights.  Errors: EINET_ERR_INVALID_ARG (top < 1, n < 0,
+ * n * top above 2^31 - 1, negative sizes, out_stride_bytes < row_bytes, NULL pointers), EINET_ERR_HIP. */
+int einet_dispatch(const void* row_dev, int64_t row_bytes, int64_t row_stride_bytes, int64_t n, int top,
+                   const int32_t* place_dev, void* out_dev, int64_t out_stride_bytes, int64_t out_rows, void* stream);
+
+/* Rows back from their components: out[i] = sum_s weight[i][s] * row[place[i][s]] over the slots with a position in
+ * 0..n_rows-1 (zeros where there is none), summed in float32 in the order of the slots and rounded once.
+ *   row_dev     device, [n_rows][width] of `dtype`, rows row_stride elements apart
+ *   place_dev   device, [n][top] int32;  weight_dev  device, [n][top] float32, or NULL: all one
+ *   out_dev     device, [n][width] of `dtype`, rows out_stride elements apart, written completely
+ * Errors as einet_dispatch, and unknown dtype. */
+int einet_combine(const void* row_dev, int dtype, int64_t width, int64_t row_stride, int64_t n_rows,
+                  const int32_t* place_dev, const float* weight_dev, int64_t n, int top, void* out_dev, int64_t out_stride,
+                  void* stream);
+
+/* Gradient of einet_combine: for every slot with a position p in 0..n_rows-1
+ *   drow[p] = weight[i][s] * dout[i],  dweight[i][s] = sum_k dout[i][k] * row[p][k]  (float32 sums)
+ * and dweight = 0 for the others.  Rows of drow_dev that no slot has are left as they were.
+ *   dout_dev  device, [n][width] of `dtype`, rows dout_stride elements apart
+ *   drow_dev  device, [n_rows][width] of `dtype`, rows drow_stride elements apart;  dweight_dev  device, [n][top] float32
+ * Different slots must have different positions; drow_dev must not overlap row_dev or dout_dev.  Errors as einet_combine. */
+int einet_combine_backward(const void* dout_dev, int64_t dout_stride, const void* row_dev, int dtype, int64_t width,
+                           int64_t row_stride, int64_t n_rows, const int32_t* place_dev, const float* weight_dev, int64_t n,
+                           int top, void* drow_dev, int64_t drow_stride, float* dweight_dev, void* stream);
+
+/* Bytes of device workspace that einet_choose needs for n_rows rows of n_entries (0 is possible).  bytes: host. */
+int einet_choose_workspace(int n_rows, int n_entries, size_t* bytes);
+
+/* One entry per row of logits, from given uniforms.  Entries at -inf or NaN are left out; the others have the weights
+ * exp((logit - largest) / temperature) (next to an entry at +inf only those at +inf have any) and the order (logit
+ * descending, index ascending).  Kept are, one filter after the other:
+ *   top_k   the first top_k entries of the order (0: all)
+ *   top_p   of those the entries with less than top_p of their total weight before them, and always the first (1: all)
+ *   min_p   of those the entries with at least min_p times the largest weight (0: all)
+ * The choice is the first index, ascending, whose running sum of kept weights exceeds u times their total: what
+ * einet_sample does with weights, here from their logarithms.  temperature 0: the first entry of the order, whatever
+ * the filters.  Weights are summed as whole multiples of 2^-(62 - ceil(log2 n_entries)) of the largest, exactly.
+ *   logit_dev   device, [n_rows][n_entries] of `dtype`, rows row_stride elements apart (0: the same row for all)
+ *   u_dev       device, [n_rows] float32 in [0,1) (below 0 or NaN counts as 0, from 1 on as the last kept entry)
+ *   temperature_dev, top_k_dev, top_p_dev, min_p_dev   device, [n_rows] settings of every row, or NULL: then the value
+ *               behind the pointer holds for all rows.  On the device a temperature that is not above 0 is 0, a top_k
+ *               below 1 is 0, top_p below 0 is 0 and NaN 1, min_p below 0 or NaN is 0 and above 1 is 1.
+ *   index_dev   device, [n_rows] int32, written: -1 for a row whose entries are all left out
+ *   logq_dev    device, [n_rows] float32, written, or NULL: log of the chosen entry's share of the kept weight, -inf for -1
+ *   workspace_dev   device, einet_choose_workspace bytes, 256-byte aligned (NULL if that is 0)
+ * n_rows = 0 does nothing.  Errors: EINET_ERR_INVALID_ARG (unknown dtype, n_rows < 0, n_entries < 1, a value for all rows out of
+ * range: temperature below 0, top_k below 0, top_p or min_p outside [0, 1]; pointers, workspace), EINET_ERR_HIP. */
+int einet_choose(const void* logit_dev, int dtype, int64_t row_stride, int n_rows, int n_entries, const float* u_dev,
+                 const float* temperature_dev, float temperature, const int32_t* top_k_dev, int top_k,
+                 const float* top_p_dev, float top_p, const float* min_p_dev, float min_p, int32_t* index_dev,
+                 float* logq_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
+
 /* Per-kernel timing for benchmarks (no passage of the paper: measurement aid).
  * While enabled, every kernel launch of the compute calls above is bracketed
  * by two HIP events recorded on the call's stream.  einet_profile_read

@@ -16,7 +16,8 @@ EXPORTED_SYMBOLS = [
     "einet_create", "einet_destroy", "einet_last_error", "einet_sizes", "einet_structure", "einet_bind",
     "einet_refresh", "einet_init_params", "einet_logp", "einet_logp_static", "einet_em_accumulate", "einet_em_update", "einet_em_reset", "einet_em_epoch",
     "einet_mixture_logp", "einet_sample", "einet_profile_enable", "einet_profile_read", "einet_profile_launches",
-    "einet_measure_peaks",
+    "einet_measure_peaks", "einet_route", "einet_route_workspace", "einet_route_backward", "einet_sort_workspace", "einet_sort",
+    "einet_dispatch", "einet_combine", "einet_combine_backward", "einet_choose_workspace", "einet_choose",
 ]
 
 
@@ -83,6 +84,17 @@ def load_library():
     lib.einet_profile_launches.argtypes = [vp, C.c_int64, C.POINTER(C.c_int64), C.POINTER(i32), C.POINTER(f32),
                                            C.POINTER(C.c_int64)]
     lib.einet_measure_peaks.argtypes = [vp, vp, C.c_int64, i32, C.POINTER(C.c_double), vp]
+    i64, size, psize = C.c_int64, C.c_size_t, C.POINTER(C.c_size_t)
+    lib.einet_route.argtypes = [vp, i32, i64, i64, vp, i32, i64, i32, i32, vp, vp, vp, vp]
+    lib.einet_route_workspace.argtypes = [i32, i64, psize]
+    lib.einet_route_backward.argtypes = [vp, i32, i64, i64, vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, i64, i64, vp, vp, size, vp]
+    lib.einet_sort_workspace.argtypes = [i64, i32, psize]
+    lib.einet_sort.argtypes = [vp, i64, i32, vp, vp, vp, size, vp]
+    lib.einet_dispatch.argtypes = [vp, i64, i64, i64, i32, vp, vp, i64, i64, vp]
+    lib.einet_combine.argtypes = [vp, i32, i64, i64, i64, vp, vp, i64, i32, vp, i64, vp]
+    lib.einet_combine_backward.argtypes = [vp, i64, vp, i32, i64, i64, i64, vp, vp, i64, i32, vp, i64, vp, vp]
+    lib.einet_choose_workspace.argtypes = [i32, i32, psize]
+    lib.einet_choose.argtypes = [vp, i32, i64, i32, i32, vp, vp, f32, vp, i32, vp, f32, vp, f32, vp, vp, vp, size, vp]
     _lib = lib
     return lib
 
@@ -409,6 +421,211 @@ def einet_mixture_logp(component_logp, log_coef, out=None):
     if rc != 0:
         raise EinetError(rc, lib.einet_last_error(None).decode())
     return out
+
+
+# ---- routing samples to the components of a mixture, and choices from logits (no handle)
+
+_ROW_TYPES = {}
+
+
+def _row_type(t):
+    """The C number of a tensor's element type."""
+    if not _ROW_TYPES:
+        import torch
+        _ROW_TYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    assert t.dtype in _ROW_TYPES, f"float32, bfloat16 or float16 is needed, got {t.dtype}"
+    return _ROW_TYPES[t.dtype]
+
+
+def _on(device, dtype, shape, *tensors):
+    """The C ABI sees pointers only: every tensor must be a contiguous one of this type and shape on this device."""
+    for t in tensors:
+        assert t is None or (t.dtype == dtype and t.device == device and tuple(t.shape) == tuple(shape) and t.is_contiguous()), \
+            f"a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is needed, got {t.dtype} {tuple(t.shape)} on {t.device}"
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _enqueue(name, device, *args):
+    """Calls a C function without a handle on the current stream of `device`."""
+    import torch
+    lib = load_library()
+    if device.index == torch.cuda.current_device():
+        rc = getattr(lib, name)(*args, torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            rc = getattr(lib, name)(*args, torch.cuda.current_stream().cuda_stream)
+    if rc != 0:
+        raise EinetError(rc, lib.einet_last_error(None).decode())
+
+
+def _workspace(name, device, *sizes):
+    import torch
+    lib = load_library()
+    n = C.c_size_t()
+    rc = getattr(lib, name)(*sizes, C.byref(n))
+    if rc != 0:
+        raise EinetError(rc, lib.einet_last_error(None).decode())
+    return (torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None), n.value
+
+
+def _scores(scores, log_coef):
+    import torch
+    assert scores.is_cuda and scores.dim() == 2, "scores must be a cuda tensor [n_components, n]"
+    if log_coef is not None:
+        _on(scores.device, torch.float32, scores.shape[:1], log_coef)
+    return (scores.data_ptr(), _row_type(scores), scores.stride(0), scores.stride(1), _ptr(log_coef)) + tuple(scores.shape)
+
+
+def einet_route(scores, log_coef=None, top=1, renormalise=False):
+    """The `top` most probable components of every sample.  scores: cuda [n_components, n] float32, bfloat16 or float16
+    with any strides (log-densities as in einet_mixture_logp; a router's logits [n, n_components] as their transposed
+    view); log_coef: cuda float32 [n_components] or None.  Returns ids int32 [n, top] (-1 where no component is left),
+    weights float32 [n, top] (posteriors, or with `renormalise` their shares) and logp float32 [n], the mixture's
+    log-density."""
+    import torch
+    args = _scores(scores, log_coef)
+    n, device = scores.shape[1], scores.device
+    ids = torch.empty(n, top, dtype=torch.int32, device=device)
+    weights = torch.empty(n, top, dtype=torch.float32, device=device)
+    logp = torch.empty(n, dtype=torch.float32, device=device)
+    _enqueue("einet_route", device, *args, top, 1 if renormalise else 0, ids.data_ptr(), weights.data_ptr(), logp.data_ptr())
+    return ids, weights, logp
+
+
+def einet_route_backward(scores, log_coef, ids, weights, dweights=None, dlogp=None, renormalise=False):
+    """Gradient of einet_route: (dscores, like scores; dlog_coef float32 [n_components]).  dweights: float32 [n, top] or None;
+    dlogp: float32 [n] or None.  With dweights None and dlogp = 1 these are the posteriors of the components and their sums
+    over the samples, the E-step of the mixture (ids and weights may be None then)."""
+    import torch
+    args = _scores(scores, log_coef)
+    (M, n), device = scores.shape, scores.device
+    assert dweights is None or (ids is not None and weights is not None), "dweights needs ids and weights"
+    top = 1 if ids is None else ids.shape[1]
+    _on(device, torch.int32, (n, top), ids)
+    _on(device, torch.float32, (n, top), weights, dweights)
+    _on(device, torch.float32, (n,), dlogp)
+    # (laid out like the scores where those are dense; a broadcast view has no memory of its own)
+    dscores = torch.empty_like(scores)
+    dlog_coef = torch.empty(M, dtype=torch.float32, device=device)
+    ws, n_bytes = _workspace("einet_route_workspace", device, M, n)
+    _enqueue("einet_route_backward", device, *args, top, 1 if renormalise else 0, _ptr(ids), _ptr(weights), _ptr(dweights),
+             _ptr(dlogp), dscores.data_ptr(), dscores.stride(0), dscores.stride(1), dlog_coef.data_ptr(), _ptr(ws), n_bytes)
+    return dscores, dlog_coef
+
+
+def einet_sort(ids, n_components):
+    """Stable sort of slots by component.  ids: cuda int32, any shape (a value outside 0..n_components-1 goes nowhere).
+    Returns first int32 [n_components + 1] and place int32 like ids: component c has the positions first[c] .. first[c+1]-1."""
+    import torch
+    assert ids.is_cuda
+    _on(ids.device, torch.int32, ids.shape, ids)
+    place = torch.empty_like(ids)
+    first = torch.empty(n_components + 1, dtype=torch.int32, device=ids.device)
+    ws, n_bytes = _workspace("einet_sort_workspace", ids.device, ids.numel(), n_components)
+    _enqueue("einet_sort", ids.device, ids.data_ptr(), ids.numel(), n_components, first.data_ptr(), place.data_ptr(), _ptr(ws),
+             n_bytes)
+    return first, place
+
+
+def _rows(t, what):
+    """(rows, width, stride between rows) of a tensor whose rows are dense."""
+    assert t.is_cuda and t.dim() >= 2, f"{what} must be a cuda tensor of rows"
+    width, want = 1, 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        assert size <= 1 or stride == want, f"every row of {what} must be contiguous"
+        want *= size
+        width *= size
+    return t.shape[0], width, t.stride(0) if t.shape[0] > 1 else width
+
+
+def _slots(place, n, device):
+    import torch
+    assert place.dim() == 2 and place.shape[0] == n, "place must have a row for every sample"
+    _on(device, torch.int32, place.shape, place)
+    return place.shape[1]
+
+
+def einet_dispatch(x, place, out=None):
+    """Rows to their components: out[place[i, s]] = x[i].  x: cuda [n, ...] of any type, each row contiguous; place: int32
+    [n, top] from einet_sort; out: [rows, ...] like x, default a new one of n * top rows.  Rows of out that no slot has are
+    left as they were (unspecified in a new one).  The gradient of x is einet_combine(gradient of out, place)."""
+    import torch
+    n, width, stride = _rows(x, "x")
+    top = _slots(place, n, x.device)
+    if out is None:
+        out = torch.empty((n * top,) + tuple(x.shape[1:]), dtype=x.dtype, device=x.device)
+    assert out.dtype == x.dtype and out.device == x.device and out.shape[1:] == x.shape[1:]
+    rows, _, out_stride = _rows(out, "out")
+    e = x.element_size()
+    _enqueue("einet_dispatch", x.device, x.data_ptr(), width * e, stride * e, n, top, place.data_ptr(), out.data_ptr(),
+             out_stride * e, rows)
+    return out
+
+
+def einet_combine(rows, place, weights=None, out=None):
+    """Rows back from their components: out[i] = sum_s weights[i, s] * rows[place[i, s]].  rows: cuda [m, ...] float32, bfloat16
+    or float16, each row contiguous; place: int32 [n, top]; weights: float32 [n, top] or None for ones."""
+    import torch
+    m, width, stride = _rows(rows, "rows")
+    n = place.shape[0]
+    top = _slots(place, n, rows.device)
+    _on(rows.device, torch.float32, place.shape, weights)
+    if out is None:
+        out = torch.empty((n,) + tuple(rows.shape[1:]), dtype=rows.dtype, device=rows.device)
+    assert out.dtype == rows.dtype and out.device == rows.device and out.shape[1:] == rows.shape[1:] and out.shape[0] == n
+    out_stride = _rows(out, "out")[2]
+    _enqueue("einet_combine", rows.device, rows.data_ptr(), _row_type(rows), width, stride, m, place.data_ptr(), _ptr(weights), n,
+             top, out.data_ptr(), out_stride)
+    return out
+
+
+def einet_combine_backward(dout, rows, place, weights, out=None):
+    """Gradient of einet_combine with weights: (drows, like rows; dweights float32 [n, top]).  dout: [n, ...]; out: where to write
+    drows, whose rows that no slot has are left as they were (unspecified in a new one)."""
+    import torch
+    m, width, stride = _rows(rows, "rows")
+    n = place.shape[0]
+    top = _slots(place, n, rows.device)
+    _on(rows.device, torch.float32, place.shape, weights)
+    assert dout.dtype == rows.dtype and dout.device == rows.device and tuple(dout.shape) == (n,) + tuple(rows.shape[1:])
+    dout_stride = _rows(dout, "dout")[2]
+    if out is None:
+        out = torch.empty(tuple(rows.shape), dtype=rows.dtype, device=rows.device)
+    assert out.dtype == rows.dtype and out.device == rows.device and out.shape == rows.shape
+    out_stride = _rows(out, "out")[2]
+    dweights = torch.empty(place.shape, dtype=torch.float32, device=rows.device)
+    _enqueue("einet_combine_backward", rows.device, dout.data_ptr(), dout_stride, rows.data_ptr(), _row_type(rows), width, stride, m,
+             place.data_ptr(), weights.data_ptr(), n, top, out.data_ptr(), out_stride, dweights.data_ptr())
+    return out, dweights
+
+
+def einet_choose(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """One entry per row of logits.  logits: cuda [n, entries] float32, bfloat16 or float16, each row contiguous (rows may be the
+    same one, expanded); u: float32 [n] uniforms in [0, 1); temperature, top_p, min_p: a number for all rows or float32 [n];
+    top_k: an int or int32 [n].  temperature 0 takes the largest, top_k 0, top_p 1 and min_p 0 filter nothing.  Returns the
+    index int32 [n] (-1 for a row without a finite entry) and the log of its probability among what was kept, float32 [n]."""
+    import torch
+    assert logits.is_cuda and logits.dim() == 2
+    n, V = logits.shape
+    device = logits.device
+    assert V <= 1 or logits.stride(1) == 1, "every row of logits must be contiguous"
+    _on(device, torch.float32, (n,), u)
+    settings = []
+    for v, dtype in ((temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32), (min_p, torch.float32)):
+        if torch.is_tensor(v):
+            _on(device, dtype, (n,), v)
+            settings += [v.data_ptr(), 0]
+        else:
+            settings += [None, v]
+    index = torch.empty(n, dtype=torch.int32, device=device)
+    logq = torch.empty(n, dtype=torch.float32, device=device)
+    ws, n_bytes = _workspace("einet_choose_workspace", device, n, V)
+    _enqueue("einet_choose", device, logits.data_ptr(), _row_type(logits), logits.stride(0), n, V, u.data_ptr(), *settings,
+             index.data_ptr(), logq.data_ptr(), _ptr(ws), n_bytes)
+    return index, logq
 
 
 def einet_profile_enable(m, enable=True):

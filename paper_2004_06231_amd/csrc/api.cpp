@@ -205,6 +205,8 @@ void forward(einet_t* h, const Arena& ar, const float* x, const uint8_t* mask, i
 
 }  // namespace
 
+int einet_impl::fail_without_handle(int code, const std::string& why) { return fail(nullptr, code, why); }
+
 extern "C" {
 
 int einet_create(const einet_spec* spec, einet_t** out) {

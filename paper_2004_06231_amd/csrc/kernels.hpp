@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <cstdint>
+#include <string>
 
 #include "../../include/einet.h"
 
@@ -384,6 +385,9 @@ hipError_t static_scratch_address(void** ptr);
 // and with four waves per SIMD) of the current device, best of `reps` launches each; dst also receives the loops'
 // results (it needs at least EINET_PEAKS_MIN_BYTES bytes).
 hipError_t measure_peaks(const void* src, void* dst, size_t bytes, int reps, double* out, hipStream_t s);
+
+// Notes down the reason of an error of a call that has no handle (einet_last_error(NULL)) and returns `code`.
+int fail_without_handle(int code, const std::string& why);
 
 void launch_mixture_logp(const float* lp, const float* log_coef, int n_components, int B, float* out, hipStream_t s);
 
