@@ -12,7 +12,9 @@ Tolerances.  u = 2^-24 is half a step of float32.
   combine   top products and additions in float32: u (top + 2) of the sum of magnitudes, and half a step of the type.
   dweights  products and sums over a row of H: at most H / 64 + 64 additions in a lane and 16 across: u (H / 64 + 82) of
             the sum of magnitudes.
-  choose    the index is the oracle's; its log-share comes from float64 and sums that are exact to 2^-40: u |logq| + 2^-36.
+  choose    the index is the oracle's; its log-share comes from float64 numbers (2^-36 for their sums and logarithms, which stay
+            below 2^7) and from a total of V weights, each rounded to a multiple of 2^-(62 - ceil(log2 V)) of the largest: off
+            by V / 2 such units of a total of one at least, rounded once: u |logq| + 2^-36 + V 2^-(63 - ceil(log2 V)).
 """
 import math
 
@@ -259,7 +261,8 @@ def check_choose(logits, u, **settings):
     want = [R.choose(x[b], uu[b], **{k: (int(v[b]) if k == "top_k" else float(v[b])) for k, v in each.items()}) for b in range(len(uu))]
     assert host(index).tolist() == [i for i, _ in want]
     q = np.array([v for _, v in want])
-    close(logq, q, U * np.where(np.isfinite(q), np.abs(q), 0) + 2.0 ** -36)
+    V = x.shape[1]
+    close(logq, q, U * np.where(np.isfinite(q), np.abs(q), 0) + 2.0 ** -36 + V * 2.0 ** -(63 - (V - 1).bit_length()))
     return index
 
 
