@@ -353,7 +353,7 @@ int einet_route_workspace(int n_components, int64_t n, size_t* bytes);
  *   dscore_dev     device, written completely, of `dtype`, entry (c, i) at c * dcomponent_stride + i * dsample_stride
  *   dlog_coef_dev  device, [n_components] float32, written, or NULL; needs the workspace (einet_route_workspace bytes,
  *                  16-byte aligned)
- * The entries of dscore_dev must not share memory.  n = 0 writes zeros to dlog_coef_dev.  Errors as einet_route. */
+ * The entries of dscore_dev must share no memory with each other nor with an input.  n = 0 writes zeros to dlog_coef_dev.  Errors as einet_route. */
 int einet_route_backward(const void* score_dev, int dtype, int64_t component_stride, int64_t sample_stride,
                          const float* log_coef_dev, int n_components, int64_t n, int top, int renormalise,
                          const int32_t* id_dev, const float* weight_dev, const float* dweight_dev, const float* dlogp_dev,

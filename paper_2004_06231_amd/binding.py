@@ -452,11 +452,14 @@ def _enqueue(name, device, *args):
     """Calls a C function without a handle on the current stream of `device`."""
     import torch
     lib = load_library()
-    if device.index == torch.cuda.current_device():
-        rc = getattr(lib, name)(*args, torch.cuda.current_stream().cuda_stream)
+    index = device.index
+    # (the stream's number without a Stream object around it, which costs as much as the launch)
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    if index == torch.cuda.current_device():
+        rc = getattr(lib, name)(*args, stream)
     else:
         with torch.cuda.device(device):
-            rc = getattr(lib, name)(*args, torch.cuda.current_stream().cuda_stream)
+            rc = getattr(lib, name)(*args, stream)
     if rc != 0:
         raise EinetError(rc, lib.einet_last_error(None).decode())
 

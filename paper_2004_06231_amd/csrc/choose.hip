@@ -116,9 +116,9 @@ __device__ __forceinline__ u64 target_of(double u, u64 total) {
 // N consecutive entries of a row, of which the first `count` exist; the hardware loads them at any alignment at once
 template <class T, int N>
 __device__ __forceinline__ void load_keys(const T* x, int count, uint32_t (&k)[N]) {
-    struct __attribute__((packed, aligned(sizeof(T)))) Pack { T v[N]; };
+    struct Pack { T v[N]; };
     if (count >= N) {
-        const Pack q = *reinterpret_cast<const Pack*>(x);
+        const Pack q = load_bytes<Pack>(x);
 #pragma unroll
         for (int c = 0; c < N; ++c) k[c] = logit_key(q.v[c]);
     } else {

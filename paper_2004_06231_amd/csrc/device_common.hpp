@@ -30,6 +30,26 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 // four consecutive floats at any multiple of four bytes (the hardware's 16-byte loads need no more)
 typedef float floatx4u __attribute__((ext_vector_type(4), aligned(4)));
 
+// A plain struct of 2, 4, 8 or 16 bytes at any address, as one load or store: the hardware does these at any address.
+typedef uint16_t raw2 __attribute__((aligned(1)));
+typedef uint32_t raw4 __attribute__((aligned(1)));
+typedef uint32_t raw8 __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t raw16 __attribute__((ext_vector_type(4), aligned(1)));
+template <int BYTES> struct RawBytes;
+template <> struct RawBytes<2> { typedef raw2 type; };
+template <> struct RawBytes<4> { typedef raw4 type; };
+template <> struct RawBytes<8> { typedef raw8 type; };
+template <> struct RawBytes<16> { typedef raw16 type; };
+template <class P>
+__device__ __forceinline__ P load_bytes(const void* p) {
+    const typename RawBytes<sizeof(P)>::type r = *reinterpret_cast<const typename RawBytes<sizeof(P)>::type*>(p);
+    return __builtin_bit_cast(P, r);
+}
+template <class P>
+__device__ __forceinline__ void store_bytes(void* p, const P& v) {
+    *reinterpret_cast<typename RawBytes<sizeof(P)>::type*>(p) = __builtin_bit_cast(typename RawBytes<sizeof(P)>::type, v);
+}
+
 constexpr int EINET_NUM_CUS = 256;        // compute units of an MI355X: workgroups of a one-per-unit launch
 constexpr int EINET_MAX_DEVICES = 16;     // per-device once-flags of the launchers
 

@@ -10,90 +10,208 @@ namespace {
 template <class T>
 __device__ __forceinline__ float to_float(T v) { return (float)v; }
 
-template <int G>
-__device__ __forceinline__ double group_max(double v) {
-#pragma unroll
-    for (int o = G / 2; o >= 1; o >>= 1) v = fmax(v, __shfl_xor(v, o, G));
-    return v;
-}
-template <int G>
-__device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-    for (int o = G / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, G);
-    return v;
-}
-
 // ---------------------------------------------------------------------------------------------------- routing
 //
 // With t[c] = score[c] + coef[c], m = max t and z = sum exp(t[c] - m): logp = m + log z, p[c] = exp(t[c] - m) / z.  The
-// sums t are formed in float64: log-densities are in the hundreds and thousands and differ by little, and which of two
-// is larger must not depend on a rounding.  A component whose t is -inf or NaN is left out.
-//
-// G lanes share a sample, each with E components in registers (component e * G + lane).
+// sums t are formed in float64 (type K): log-densities are in the hundreds and thousands and differ by little, and which
+// of two is larger must not depend on a rounding.  Without coefficients t is the score, and K float.  A component whose t
+// is -inf or NaN is left out.
 
-template <class T, int G, int E>
-__device__ __forceinline__ double route_load(const T* __restrict__ p, int64_t sc, int64_t sn, const float* __restrict__ coef,
-                                             int M, int64_t n, int j, double (&t)[E]) {
-    double m = -INFINITY;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const int c = e * G + j;
-        double v = -INFINITY;
-        if (c < M) {
-            v = (double)to_float(p[c * sc + n * sn]);
-            if (coef) v += (double)coef[c];
-            if (!(v > -INFINITY)) v = -INFINITY;
-        }
-        t[e] = v;
-        m = fmax(m, v);
-    }
-    return group_max<G>(m);
+// All lanes of a group of G get op over the group: lanes that differ in one, then in two bits, mirrored halves of 8 and 16.
+template <int CTRL>
+__device__ __forceinline__ float lane_of(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL>
+__device__ __forceinline__ int lane_of(int v) { return __builtin_amdgcn_mov_dpp(v, CTRL, 0xf, 0xf, true); }
+template <int CTRL>
+__device__ __forceinline__ double lane_of(double v) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)lane_of<CTRL>((int)(uint32_t)b), hi = (uint32_t)lane_of<CTRL>((int)(uint32_t)(b >> 32));
+    return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+template <int G, class V, class Op>
+__device__ __forceinline__ V group_reduce(V v, Op op) {
+    if constexpr (G >= 2) v = op(v, lane_of<0xB1>(v));
+    if constexpr (G >= 4) v = op(v, lane_of<0x4E>(v));
+    if constexpr (G >= 8) v = op(v, lane_of<0x141>(v));
+    if constexpr (G >= 16) v = op(v, lane_of<0x140>(v));
+    if constexpr (G >= 32) v = op(v, __shfl_xor(v, 16, 64));
+    if constexpr (G >= 64) v = op(v, __shfl_xor(v, 32, 64));
+    return v;
+}
+struct Larger {
+    __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
+    __device__ double operator()(double a, double b) const { return fmax(a, b); }
+};
+struct Smaller {
+    __device__ int operator()(int a, int b) const { return min(a, b); }
+};
+struct Plus {
+    __device__ float operator()(float a, float b) const { return a + b; }
+};
+
+// exp(t - m) of a component, 1 at the maximum (also where both are infinite), 0 for one that is left out.  The argument is
+// rounded to float32 once: of the product with log2(e) what its rounding took is added back to first order.
+__device__ __forceinline__ float route_exp(double t, double m) {
+    const float y = (float)fmax((t - m) * 1.4426950408889634074, -200.0);
+    return t == m ? 1.f : __builtin_amdgcn_exp2f(y);
+}
+__device__ __forceinline__ float route_exp(float t, float m) {
+    constexpr float L = 1.44269502f, L_REST = 1.92596299e-8f;
+    const float d = fmaxf(t - m, -150.f), y = d * L, e = __builtin_amdgcn_exp2f(y);
+    const float rest = fmaf(d, L_REST, fmaf(d, L, -y));
+    return t == m ? 1.f : fmaf(e, rest * 0.693147182f, e);
 }
 
-// exp(t - m) of a component, 1 at the maximum (also where both are infinite)
-__device__ __forceinline__ float route_exp(double t, double m) { return t == m ? 1.f : expf((float)(t - m)); }
+template <class K, class T>
+__device__ __forceinline__ K route_sum(T score, const float* coef, int c) {
+    K t = (K)to_float(score);
+    if constexpr (sizeof(K) == 8) t += (K)coef[c];
+    return t > (K)-INFINITY ? t : (K)-INFINITY;                 // (NaN too)
+}
 
+// G lanes share a sample, each with E components in registers: VEC neighbours of every G * VEC, which are one load where
+// the components of a sample are next to each other.
+template <class T, int E> constexpr int ROUTE_VEC = E < 16 / (int)sizeof(T) ? E : 16 / (int)sizeof(T);
 template <class T, int G, int E>
+__device__ __forceinline__ int route_component(int e, int j) {
+    constexpr int VEC = ROUTE_VEC<T, E>;
+    return ((e / VEC) * G + j) * VEC + e % VEC;
+}
+
+template <class T, class K, int G, int E>
+__device__ __forceinline__ K route_load(const T* __restrict__ p, int64_t sc, int64_t sn, const float* __restrict__ coef, int M,
+                                        int64_t n, int j, K (&t)[E]) {
+    constexpr int VEC = ROUTE_VEC<T, E>;
+    struct Pack { T v[VEC]; };
+    const T* const row = p + n * sn;
+    K m = (K)-INFINITY;
+#pragma unroll
+    for (int v = 0; v < E / VEC; ++v) {
+        const int c0 = route_component<T, G, E>(v * VEC, j);
+        if (sc == 1 && c0 + VEC <= M) {
+            const Pack q = load_bytes<Pack>(row + c0);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) t[v * VEC + i] = route_sum<K>(q.v[i], coef, c0 + i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                t[v * VEC + i] = c0 + i < M ? route_sum<K>(row[(c0 + i) * sc], coef, c0 + i) : (K)-INFINITY;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) m = Larger{}(m, t[e]);
+    return group_reduce<G>(m, Larger{});
+}
+
+template <class T, class K, int G, int E>
 __global__ __launch_bounds__(256) void k_route(const T* __restrict__ p, int64_t sc, int64_t sn, const float* __restrict__ coef,
                                                int M, int64_t N, int top, int renormalise, int32_t* __restrict__ ids,
                                                float* __restrict__ weights, float* __restrict__ logp) {
     const int j = threadIdx.x % G;
     const int64_t n = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
     if (n >= N) return;
-    double t[E];
-    const double m = route_load<T, G, E>(p, sc, sn, coef, M, n, j, t);
-    const bool dead = !(m > -INFINITY);
+    K t[E];
+    const K m = route_load<T, K, G, E>(p, sc, sn, coef, M, n, j, t);
+    const bool dead = !(m > (K)-INFINITY);
     float z = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) z += dead ? 0.f : route_exp(t[e], m);
-    z = group_sum<G>(z);
+    z = group_reduce<G>(z, Plus{});
     // one selection after the other, the largest of what is left; lane s of the group keeps selection s
     int my_id = -1;
     float my_e = 0.f;
+    K best = m;
     for (int s = 0; s < top; ++s) {
-        double best = -INFINITY;
+        if (s > 0) {
+            best = (K)-INFINITY;
+#pragma unroll
+            for (int e = 0; e < E; ++e) best = Larger{}(best, t[e]);
+            best = group_reduce<G>(best, Larger{});
+        }
+        if (!(best > (K)-INFINITY)) break;
         int c = 0x7fffffff;
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (t[e] > best) best = t[e], c = e * G + j;
-#pragma unroll
-        for (int o = G / 2; o >= 1; o >>= 1) {
-            const double ob = __shfl_xor(best, o, G);
-            const int oc = __shfl_xor(c, o, G);
-            if (ob > best || (ob == best && oc < c)) best = ob, c = oc;
-        }
-        if (!(best > -INFINITY)) break;
+        for (int e = E - 1; e >= 0; --e) c = t[e] == best ? route_component<T, G, E>(e, j) : c;
+        c = group_reduce<G>(c, Smaller{});
         if (j == s) my_id = c, my_e = route_exp(best, m);
 #pragma unroll
         for (int e = 0; e < E; ++e)
-            if (c == e * G + j) t[e] = -INFINITY;
+            if (c == route_component<T, G, E>(e, j)) t[e] = (K)-INFINITY;
     }
-    const float total = renormalise ? group_sum<G>(my_e) : z;
+    const float total = renormalise ? group_reduce<G>(my_e, Plus{}) : z;
     if (j < top) {
         ids[n * top + j] = my_id;
         weights[n * top + j] = my_id >= 0 ? my_e / total : 0.f;
     }
-    if (j == 0) logp[n] = dead ? -INFINITY : (float)(m + (double)logf(z));
+    if (j == 0) logp[n] = dead ? -INFINITY : (float)((double)m + (double)logf(z));
+}
+
+// A sample to a lane, for components whose samples are next to each other: the loads of a component are contiguous over
+// the lanes.  The scores are gone through twice, for the maximum with the selections and for the sum.
+constexpr int ROUTE_COLUMNS_MOST = 128;              // components: the eight running sums of z add up 16 terms at most
+template <class T, class K, int TOP>
+__global__ __launch_bounds__(256) void k_route_columns(const T* __restrict__ p, int64_t sc, const float* __restrict__ coef, int M,
+                                                       int64_t N, int top, int renormalise, int32_t* __restrict__ ids,
+                                                       float* __restrict__ weights, float* __restrict__ logp) {
+    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (n >= N) return;
+    p += n;
+    K best[TOP];
+    int id[TOP];
+#pragma unroll
+    for (int s = 0; s < TOP; ++s) best[s] = (K)-INFINITY, id[s] = -1;
+    for (int c0 = 0; c0 < M; c0 += 8) {
+        T x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = p[min(c0 + i, M - 1) * sc];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = c0 + i;
+            K t = c < M ? route_sum<K>(x[i], coef, min(c, M - 1)) : (K)-INFINITY;
+            if (!(t > best[TOP - 1])) continue;              // (equal ones stay behind the lower component)
+            best[TOP - 1] = t;
+            id[TOP - 1] = c;
+#pragma unroll
+            for (int s = TOP - 1; s > 0; --s)
+                if (best[s] > best[s - 1]) {
+                    const K b = best[s];
+                    const int k = id[s];
+                    best[s] = best[s - 1], id[s] = id[s - 1];
+                    best[s - 1] = b, id[s - 1] = k;
+                }
+        }
+    }
+    const K m = best[0];
+    const bool dead = !(m > (K)-INFINITY);
+    float sums[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[i] = 0.f;
+    if (!dead)
+        for (int c0 = 0; c0 < M; c0 += 8) {
+            T x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = p[min(c0 + i, M - 1) * sc];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c0 + i < M) sums[i] += route_exp(route_sum<K>(x[i], coef, c0 + i), m);
+        }
+    const float z = ((sums[0] + sums[1]) + (sums[2] + sums[3])) + ((sums[4] + sums[5]) + (sums[6] + sums[7]));
+    float e[TOP], total = 0.f;
+#pragma unroll
+    for (int s = 0; s < TOP; ++s) {
+        e[s] = s < top && best[s] > (K)-INFINITY ? route_exp(best[s], m) : 0.f;
+        total += e[s];
+    }
+    if (!renormalise) total = z;
+#pragma unroll
+    for (int s = 0; s < TOP; ++s)
+        if (s < top) {
+            ids[n * top + s] = id[s];
+            weights[n * top + s] = id[s] >= 0 ? e[s] / total : 0.f;
+        }
+    logp[n] = dead ? -INFINITY : (float)((double)m + (double)logf(z));
 }
 
 // With a = sum_s dw[s] w[s]:
@@ -102,14 +220,15 @@ __global__ __launch_bounds__(256) void k_route(const T* __restrict__ p, int64_t 
 // The log-density and the weights are differences and quotients of numbers rounded to float32; m and z come from the
 // scores again.  d coef[c] = sum_n d t[c][n]: a lane has the same components for all its samples and adds their gradients
 // up in registers; the workgroup's sums go to a row of the workspace, which the second kernel adds up in a fixed order.
-template <class T, int G, int E>
+template <class T, class K, int G, int E>
 __global__ __launch_bounds__(256) void k_route_backward(const T* __restrict__ p, int64_t sc, int64_t sn,
                                                         const float* __restrict__ coef, int M, int64_t N, int top,
                                                         int renormalise, const int32_t* __restrict__ ids,
                                                         const float* __restrict__ weights, const float* __restrict__ dweights,
                                                         const float* __restrict__ dlogp, T* __restrict__ dscores, int64_t dsc,
                                                         int64_t dsn, float* __restrict__ partial) {
-    constexpr int S = 256 / G;
+    constexpr int S = 256 / G, VEC = ROUTE_VEC<T, E>;
+    struct Pack { T v[VEC]; };
     const int j = threadIdx.x % G;
     float acc[E];
 #pragma unroll
@@ -117,9 +236,9 @@ __global__ __launch_bounds__(256) void k_route_backward(const T* __restrict__ p,
     for (int64_t n0 = (int64_t)blockIdx.x * S; n0 < N; n0 += (int64_t)gridDim.x * S) {
         const int64_t n = n0 + threadIdx.x / G;
         if (n >= N) continue;                                   // (whole groups leave together)
-        double t[E];
-        const double m = route_load<T, G, E>(p, sc, sn, coef, M, n, j, t);
-        const bool dead = !(m > -INFINITY);
+        K t[E];
+        const K m = route_load<T, K, G, E>(p, sc, sn, coef, M, n, j, t);
+        const bool dead = !(m > (K)-INFINITY);
         float z = 0.f;
         float d[E];
 #pragma unroll
@@ -127,7 +246,7 @@ __global__ __launch_bounds__(256) void k_route_backward(const T* __restrict__ p,
             d[e] = dead ? 0.f : route_exp(t[e], m);
             z += d[e];
         }
-        z = group_sum<G>(z);
+        z = group_reduce<G>(z, Plus{});
         int id = -1;
         float w = 0.f, dw = 0.f;
         if (j < top && dweights) {
@@ -136,7 +255,7 @@ __global__ __launch_bounds__(256) void k_route_backward(const T* __restrict__ p,
             dw = dweights[n * top + j];
             if (id < 0) w = dw = 0.f;
         }
-        const float a = group_sum<G>(w * dw), dl = dlogp ? dlogp[n] : 0.f;
+        const float a = group_reduce<G>(w * dw, Plus{}), dl = dlogp ? dlogp[n] : 0.f;
         const float scale = dead ? 0.f : (renormalise ? dl : dl - a) / z, add = w * (renormalise ? dw - a : dw);
 #pragma unroll
         for (int e = 0; e < E; ++e) d[e] *= scale;
@@ -146,14 +265,25 @@ __global__ __launch_bounds__(256) void k_route_backward(const T* __restrict__ p,
                 const float v = __shfl(add, s, G);
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    if (c == e * G + j) d[e] += v;
+                    if (c == route_component<T, G, E>(e, j)) d[e] += v;
             }
+        T* const row = dscores + n * dsn;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int c = e * G + j;
-            if (c < M) dscores[c * dsc + n * dsn] = (T)d[e];
-            acc[e] += d[e];
+        for (int v = 0; v < E / VEC; ++v) {
+            const int c0 = route_component<T, G, E>(v * VEC, j);
+            if (dsc == 1 && c0 + VEC <= M) {
+                Pack q;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) q.v[i] = (T)d[v * VEC + i];
+                store_bytes(row + c0, q);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    if (c0 + i < M) row[(c0 + i) * dsc] = (T)d[v * VEC + i];
+            }
         }
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] += d[e];
     }
     if (!partial) return;
     __shared__ float sums[4][G * E];
@@ -162,37 +292,130 @@ __global__ __launch_bounds__(256) void k_route_backward(const T* __restrict__ p,
         float v = acc[e];
 #pragma unroll
         for (int o = 32; o >= G; o >>= 1) v += __shfl_xor(v, o, 64);
-        if ((threadIdx.x & 63) < G) sums[threadIdx.x >> 6][e * G + j] = v;
+        if ((threadIdx.x & 63) < G) sums[threadIdx.x >> 6][route_component<T, G, E>(e, j)] = v;
     }
     __syncthreads();
     for (int c = threadIdx.x; c < M; c += 256)
         partial[(size_t)blockIdx.x * M + c] = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
 }
 
-// dcoef[c] = sum of the rows of `partial`, in float64: 64 columns and four interleaved shares of the rows per workgroup
-__global__ __launch_bounds__(256) void k_route_coef(const float* __restrict__ partial, int rows, int M, float* __restrict__ dcoef) {
-    __shared__ double sums[4][64];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), share = threadIdx.x >> 6;
-    double v = 0.0;
-    if (c < M)
-        for (int r = share; r < rows; r += 4) v += (double)partial[(size_t)r * M + c];
-    sums[share][threadIdx.x & 63] = v;
+// The same with a sample to a lane.  The gradients of a component are added up over the lanes of a wave as they arise.
+template <class T, class K>
+__global__ __launch_bounds__(256) void k_route_backward_columns(const T* __restrict__ p, int64_t sc, const float* __restrict__ coef,
+                                                                int M, int64_t N, int top, int renormalise,
+                                                                const int32_t* __restrict__ ids, const float* __restrict__ weights,
+                                                                const float* __restrict__ dweights, const float* __restrict__ dlogp,
+                                                                T* __restrict__ dscores, int64_t dsc, float* __restrict__ partial) {
+    __shared__ float sums[4][ROUTE_COLUMNS_MOST];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int c = lane; c < M; c += 64) sums[wave][c] = 0.f;     // (a wave's own, by lane 63 only from here on)
     __syncthreads();
-    if (share == 0 && c < M) dcoef[c] = (float)((sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]));
+    for (int64_t n0 = (int64_t)blockIdx.x * 256; n0 < N; n0 += (int64_t)gridDim.x * 256) {
+        const bool there = n0 + threadIdx.x < N;
+        const int64_t n = there ? n0 + threadIdx.x : N - 1;
+        const T* const x = p + n;
+        K m = (K)-INFINITY;
+        for (int c0 = 0; c0 < M; c0 += 8) {
+            T v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = x[min(c0 + i, M - 1) * sc];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = Larger{}(m, route_sum<K>(v[i], coef, min(c0 + i, M - 1)));
+        }
+        const bool dead = !(m > (K)-INFINITY);
+        float part[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part[i] = 0.f;
+        for (int c0 = 0; c0 < M; c0 += 8) {
+            T v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = x[min(c0 + i, M - 1) * sc];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c0 + i < M) part[i] += dead ? 0.f : route_exp(route_sum<K>(v[i], coef, c0 + i), m);
+        }
+        const float z = ((part[0] + part[1]) + (part[2] + part[3])) + ((part[4] + part[5]) + (part[6] + part[7]));
+        int id[4];
+        float add[4], a = 0.f;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            id[s] = s < top && dweights ? ids[n * top + s] : -1;
+            add[s] = id[s] >= 0 ? weights[n * top + s] * dweights[n * top + s] : 0.f;
+            a += add[s];
+        }
+        if (renormalise) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                if (id[s] >= 0) add[s] = weights[n * top + s] * (dweights[n * top + s] - a);
+        }
+        const float dl = dlogp ? dlogp[n] : 0.f;
+        const float scale = dead ? 0.f : (renormalise ? dl : dl - a) / z;
+        for (int c0 = 0; c0 < M; c0 += 8) {
+            T v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = x[min(c0 + i, M - 1) * sc];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = c0 + i;
+                if (c >= M) break;
+                float d = dead ? 0.f : route_exp(route_sum<K>(v[i], coef, c), m) * scale;
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+                    if (id[s] == c) d += add[s];
+                if (there) dscores[c * dsc + n] = (T)d;
+                if (partial) {
+                    float r = there ? d : 0.f;
+                    r += lane_of<0xB1>(r);
+                    r += lane_of<0x4E>(r);
+                    r += lane_of<0x141>(r);
+                    r += lane_of<0x140>(r);
+                    r += __shfl_xor(r, 16, 64);
+                    r += __shfl_xor(r, 32, 64);
+                    if (lane == 63) sums[wave][c] += r;
+                }
+            }
+        }
+    }
+    if (!partial) return;
+    __syncthreads();
+    for (int c = threadIdx.x; c < M; c += 256)
+        partial[(size_t)blockIdx.x * M + c] = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
+}
+
+// dcoef[c] = sum of the rows of `partial`, in float64: a workgroup has 32 columns and 32 interleaved shares of the rows
+__global__ __launch_bounds__(1024) void k_route_coef(const float* __restrict__ partial, int rows, int M, float* __restrict__ dcoef) {
+    __shared__ double sums[32][33];
+    const int x = threadIdx.x & 31, share = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
+    double v = 0.0;
+    if (c < M) {
+#pragma unroll 8
+        for (int r = share; r < rows; r += 32) v += (double)partial[(size_t)r * M + c];
+    }
+    sums[share][x] = v;
+    __syncthreads();
+    if (share == 0 && c < M) {
+        double d = 0.0;
+        for (int r = 0; r < 32; ++r) d += sums[r][x];
+        dcoef[c] = (float)d;
+    }
 }
 
 // Lanes per sample: as many as selections at least, and at most 16 components to a lane.
 int route_lanes(int M, int top) {
+    const int most = M <= 32 ? 4 : M <= 64 ? 4 : M <= 128 ? 8 : 16;   // components to a lane
     int G = 4;
-    while (G < 64 && (G < top || G * 4 < M)) G *= 2;
+    while (G < 64 && (G < top || G * most < M)) G *= 2;
     return G;
 }
 
-constexpr int ROUTE_BACKWARD_GROUPS = 1024;          // workgroups of the gradient, which is the rows of its workspace
-int route_backward_groups(int M, int64_t N) {
+// A sample to a lane: where the samples of a component are next to each other and there are enough of them for every
+// compute unit to have two workgroups' worth of lanes.
+bool route_by_columns(const Scores& a, int top) { return a.sn == 1 && a.M <= ROUTE_COLUMNS_MOST && top <= 4 && a.N >= 2 * 256 * EINET_NUM_CUS; }
+
+// Workgroups of the gradient, which is the rows of its workspace.
+int route_backward_groups(int64_t N) {
     const int64_t tiles = (N + 3) / 4;               // (a workgroup has four samples at least)
-    (void)M;
-    return (int)(tiles < ROUTE_BACKWARD_GROUPS ? tiles : ROUTE_BACKWARD_GROUPS);
+    return (int)(tiles < 2 * EINET_NUM_CUS ? tiles : 2 * EINET_NUM_CUS);
 }
 
 // f(std::integral_constant<int, G>, std::integral_constant<int, E>) for the lanes and components per lane of M, top
@@ -202,10 +425,10 @@ void route_variant(int M, int top, F&& f) {
 #define EINET_E(GG, EE) if (E <= EE) { f(std::integral_constant<int, GG>{}, std::integral_constant<int, EE>{}); return; }
     switch (G) {
     case 4: EINET_E(4, 2) EINET_E(4, 4) return;
-    case 8: EINET_E(8, 1) EINET_E(8, 4) return;
-    case 16: EINET_E(16, 1) EINET_E(16, 4) return;
-    case 32: EINET_E(32, 4) return;
-    case 64: EINET_E(64, 4) EINET_E(64, 8) EINET_E(64, 16) return;
+    case 8: EINET_E(8, 4) return;
+    case 16: EINET_E(16, 4) EINET_E(16, 8) EINET_E(16, 16) return;
+    case 32: EINET_E(32, 16) return;
+    case 64: EINET_E(64, 16) return;
     }
 #undef EINET_E
 }
@@ -221,8 +444,22 @@ void with_type(int type, F&& f) {
 // ------------------------------------------------------------------------------------------------------- sorting
 //
 // Stable counting sort of slots by component: first[c] slots belong to components below c, place[i] is slot i's position,
-// -1 for a slot without a component.  Wave w of the workgroup has the w-th stretch of the slots.
+// -1 for a slot without a component.  Block b has the b-th stretch of the slots and wave w of it the w-th stretch of that.
+// A slot's position: the slots of lower components, those of its own in the blocks and waves before, and its rank among
+// those of the wave.  Few slots are one workgroup's; more are counted in a first launch, one row of counts per block.
 constexpr int SORT_WAVES = 16;
+constexpr int SORT_ONE_BLOCK = 4096, SORT_MOST_BLOCKS = 64;
+
+int sort_blocks(int64_t slots) {
+    if (slots <= SORT_ONE_BLOCK) return 1;
+    const int64_t b = (slots + 1023) / 1024;
+    return (int)(b < SORT_MOST_BLOCKS ? b : SORT_MOST_BLOCKS);
+}
+// slots of a block and of a wave: whole steps of a wave
+__host__ __device__ inline int64_t sort_per_wave(int64_t slots, int blocks) {
+    const int64_t waves = (int64_t)blocks * SORT_WAVES;
+    return ((slots + waves - 1) / waves + 63) & ~(int64_t)63;
+}
 
 __device__ __forceinline__ uint64_t same_key_lanes(int key, int bits) {
     uint64_t same = ~0ull;
@@ -241,23 +478,47 @@ __device__ __forceinline__ void wave_lds_fence() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+__global__ __launch_bounds__(64 * SORT_WAVES) void k_sort_count(const int32_t* __restrict__ ids, int64_t slots, int M,
+                                                                int32_t* __restrict__ counts) {
+    __shared__ int32_t count[ROUTE_MAX_COMPONENTS];
+    for (int c = threadIdx.x; c < M; c += 64 * SORT_WAVES) count[c] = 0;
+    __syncthreads();
+    const int64_t per = sort_per_wave(slots, gridDim.x) * SORT_WAVES, lo = blockIdx.x * per, hi = lo + per < slots ? lo + per : slots;
+    for (int64_t i = lo + threadIdx.x; i < hi; i += 64 * SORT_WAVES) {
+        const int c = ids[i];
+        if ((unsigned)c < (unsigned)M) atomicAdd(&count[c], 1);
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < M; c += 64 * SORT_WAVES) counts[blockIdx.x * M + c] = count[c];
+}
+
+// counts: [gridDim.x][M], not read by a single block
 __global__ __launch_bounds__(64 * SORT_WAVES) void k_sort(const int32_t* __restrict__ ids, int64_t slots, int M, int bits,
-                                                          int32_t* __restrict__ first, int32_t* __restrict__ place) {
+                                                          const int32_t* __restrict__ counts, int32_t* __restrict__ first,
+                                                          int32_t* __restrict__ place) {
     extern __shared__ int32_t count[];                       // [SORT_WAVES][M], then [SORT_WAVES] sums of the scan
     int32_t* const wave_total = count + SORT_WAVES * M;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, blocks = gridDim.x;
     for (int i = tid; i < SORT_WAVES * M; i += blockDim.x) count[i] = 0;
     __syncthreads();
-    const int64_t per = ((slots + SORT_WAVES - 1) / SORT_WAVES + 63) & ~(int64_t)63;
-    const int64_t lo = wave * per < slots ? wave * per : slots, hi = lo + per < slots ? lo + per : slots;
+    const int64_t per = sort_per_wave(slots, blocks), at0 = (blockIdx.x * (int64_t)SORT_WAVES + wave) * per;
+    const int64_t lo = at0 < slots ? at0 : slots, hi = lo + per < slots ? lo + per : slots;
     for (int64_t i = lo + lane; i < hi; i += 64) {
         const int c = ids[i];
         if ((unsigned)c < (unsigned)M) atomicAdd(&count[wave * M + c], 1);
     }
+    // thread c: the slots of component c, in all blocks and in those before this one
+    int total = 0, before_block = 0;
+    if (blocks > 1 && tid < M) {
+#pragma unroll 8
+        for (int b = 0; b < blocks; ++b) {
+            const int v = counts[b * M + tid];
+            total += v;
+            before_block += b < (int)blockIdx.x ? v : 0;
+        }
+    }
     __syncthreads();
-    // thread c: components' totals, their running sum over c, then the first position of every wave's share
-    int total = 0;
-    if (tid < M)
+    if (blocks == 1 && tid < M)
         for (int w = 0; w < SORT_WAVES; ++w) total += count[w * M + tid];
     int run = total;
 #pragma unroll
@@ -271,9 +532,11 @@ __global__ __launch_bounds__(64 * SORT_WAVES) void k_sort(const int32_t* __restr
     for (int w = 0; w < wave; ++w) before += wave_total[w];
     run += before;
     if (tid < M) {
-        first[tid] = run - total;
-        if (tid == M - 1) first[M] = run;
-        int at = run - total;
+        if (blockIdx.x == 0) {
+            first[tid] = run - total;
+            if (tid == M - 1) first[M] = run;
+        }
+        int at = run - total + before_block;
         for (int w = 0; w < SORT_WAVES; ++w) {
             const int v = count[w * M + tid];
             count[w * M + tid] = at;
@@ -297,124 +560,299 @@ __global__ __launch_bounds__(64 * SORT_WAVES) void k_sort(const int32_t* __restr
 }
 
 // ------------------------------------------------------------------------------------------- rows there and back
+//
+// A row is a number of units of up to 16 bytes (the last may be shorter; loads and stores of 16 bytes need no more than the
+// elements' alignment).  L lanes share a sample, each with UN units of every L * UN: a tile.  A tile's work is one item, so
+// that a few long rows spread over many workgroups too; rows shorter than half a wave's units share a wave.
+template <class T> constexpr int UNIT = 16 / (int)sizeof(T);
+template <class T> struct Unit { T v[UNIT<T>]; };
 
-template <class U>
-__global__ __launch_bounds__(256) void k_dispatch(const char* __restrict__ x, int64_t units, int64_t x_stride, int64_t N, int top,
-                                                  const int32_t* __restrict__ place, char* __restrict__ out, int64_t out_stride,
+template <class T>
+__device__ __forceinline__ Unit<T> load_unit(const T* p, int64_t left) {
+    if (left >= UNIT<T>) return load_bytes<Unit<T>>(p);
+    Unit<T> u;
+#pragma unroll
+    for (int i = 0; i < UNIT<T>; ++i) u.v[i] = i < left ? p[i] : T{};
+    return u;
+}
+template <class T>
+__device__ __forceinline__ void store_unit(T* p, int64_t left, const Unit<T>& u) {
+    if (left >= UNIT<T>) {
+        store_bytes(p, u);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < UNIT<T>; ++i)
+        if (i < left) p[i] = u.v[i];
+}
+
+// The item of a lane: its sample and the column of its first unit.
+template <class T, int L, int UN>
+__device__ __forceinline__ bool row_item(int64_t N, int tiles, int64_t& n, int64_t& k0) {
+    uint32_t item = blockIdx.x * (256 / L) + threadIdx.x / L;        // (N * tiles < 2^32: checked by the launcher)
+    if constexpr (L == 64) item = (uint32_t)__builtin_amdgcn_readfirstlane((int)item);
+    const uint32_t i = tiles == 1 ? item : item / (uint32_t)tiles;
+    n = i;
+    k0 = ((int64_t)(item - i * (uint32_t)tiles) * (L * UN) + threadIdx.x % L) * UNIT<T>;
+    return n < N;
+}
+
+template <class T, int L, int UN>
+__global__ __launch_bounds__(256) void k_dispatch(const T* __restrict__ x, int64_t H, int64_t x_stride, int64_t N, int tiles, int top,
+                                                  const int32_t* __restrict__ place, T* __restrict__ out, int64_t out_stride,
                                                   int64_t out_rows) {
-    const int64_t all = N * units;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        const int64_t n = i / units, k = i - n * units;
-        const U v = *reinterpret_cast<const U*>(x + n * x_stride + k * (int64_t)sizeof(U));
-        for (int s = 0; s < top; ++s) {
-            const int64_t at = place[n * top + s];
-            if (at >= 0 && at < out_rows) *reinterpret_cast<U*>(out + at * out_stride + k * (int64_t)sizeof(U)) = v;
+    int64_t n, k0;
+    if (!row_item<T, L, UN>(N, tiles, n, k0)) return;
+    Unit<T> u[UN];
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+        const int64_t k = k0 + i * L * UNIT<T>;
+        if (k < H) u[i] = load_unit(x + n * x_stride + k, H - k);
+    }
+    for (int s = 0; s < top; ++s) {
+        const int64_t at = place[n * top + s];
+        if (at < 0 || at >= out_rows) continue;
+        T* const row = out + at * out_stride;
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            const int64_t k = k0 + i * L * UNIT<T>;
+            if (k < H) store_unit(row + k, H - k, u[i]);
         }
     }
 }
 
-template <class T>
+// Slots are taken S at a time, their loads in flight together.
+template <class T, int L, int UN, int S>
 __global__ __launch_bounds__(256) void k_combine(const T* __restrict__ rows, int64_t H, int64_t stride, int64_t n_rows,
                                                  const int32_t* __restrict__ place, const float* __restrict__ weights, int64_t N,
-                                                 int top, T* __restrict__ out, int64_t out_stride) {
-    const int64_t all = N * H;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        const int64_t n = i / H, k = i - n * H;
-        float v = 0.f;
-        for (int s = 0; s < top; ++s) {
-            const int64_t at = place[n * top + s];
-            if (at >= 0 && at < n_rows) v += (weights ? weights[n * top + s] : 1.f) * to_float(rows[at * stride + k]);
+                                                 int tiles, int top, T* __restrict__ out, int64_t out_stride) {
+    int64_t n, k0;
+    if (!row_item<T, L, UN>(N, tiles, n, k0)) return;
+    float acc[UN][UNIT<T>];
+#pragma unroll
+    for (int i = 0; i < UN; ++i)
+#pragma unroll
+        for (int c = 0; c < UNIT<T>; ++c) acc[i][c] = 0.f;
+    for (int s0 = 0; s0 < top; s0 += S) {
+        Unit<T> u[S][UN];
+        float w[S];
+        bool has[S];
+#pragma unroll
+        for (int q = 0; q < S; ++q) {
+            const int64_t slot = n * top + min(s0 + q, top - 1);
+            const int64_t at = place[slot];
+            has[q] = s0 + q < top && at >= 0 && at < n_rows;
+            w[q] = weights ? weights[slot] : 1.f;
+            if (has[q]) {
+#pragma unroll
+                for (int i = 0; i < UN; ++i) {
+                    const int64_t k = k0 + i * L * UNIT<T>;
+                    if (k < H) u[q][i] = load_unit(rows + at * stride + k, H - k);
+                }
+            }
         }
-        out[n * out_stride + k] = (T)v;
+#pragma unroll
+        for (int q = 0; q < S; ++q)
+            if (has[q]) {
+#pragma unroll
+                for (int i = 0; i < UN; ++i)
+#pragma unroll
+                    for (int c = 0; c < UNIT<T>; ++c) acc[i][c] = fmaf(w[q], to_float(u[q][i].v[c]), acc[i][c]);
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+        const int64_t k = k0 + i * L * UNIT<T>;
+        Unit<T> u;
+#pragma unroll
+        for (int c = 0; c < UNIT<T>; ++c) u.v[c] = (T)acc[i][c];
+        if (k < H) store_unit(out + n * out_stride + k, H - k, u);
     }
 }
 
-template <class T>
+// The rows of a sample are gone through by L lanes (256: the whole workgroup), S slots at a time: the gradient of the
+// output is read once for them, every row once.
+template <class T, int L, int S>
 __global__ __launch_bounds__(256) void k_combine_backward(const T* __restrict__ dout, int64_t dout_stride,
                                                           const T* __restrict__ rows, int64_t H, int64_t stride, int64_t n_rows,
                                                           const int32_t* __restrict__ place, const float* __restrict__ weights,
-                                                          int64_t slots, int top, T* __restrict__ drows, int64_t drows_stride,
+                                                          int64_t N, int top, T* __restrict__ drows, int64_t drows_stride,
                                                           float* __restrict__ dweights) {
-    const int lane = threadIdx.x & 63;
-    for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < slots; i += (int64_t)gridDim.x * 4) {
-        const int64_t n = i / top, at = place[i];
-        float dot = 0.f;
-        if (at >= 0 && at < n_rows) {
-            const float w = weights[i];
-            for (int64_t k = lane; k < H; k += 64) {
-                const float g = to_float(dout[n * dout_stride + k]);
-                dot += g * to_float(rows[at * stride + k]);
-                drows[at * drows_stride + k] = (T)(w * g);
-            }
+    const int64_t n = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+    const int j = threadIdx.x % L;
+    if (n >= N) return;
+    const T* const g = dout + n * dout_stride;
+    for (int s0 = 0; s0 < top; s0 += S) {
+        int64_t at[S];
+        float w[S], dot[S];
+        bool has[S];
+#pragma unroll
+        for (int q = 0; q < S; ++q) {
+            const int64_t slot = n * top + min(s0 + q, top - 1);
+            at[q] = place[slot];
+            has[q] = s0 + q < top && at[q] >= 0 && at[q] < n_rows;
+            w[q] = weights[slot];
+            dot[q] = 0.f;
         }
-        dot = wave_sum(dot);
-        if (lane == 0) dweights[i] = dot;
+        for (int64_t k = (int64_t)j * UNIT<T>; k < H; k += L * UNIT<T>) {
+            const Unit<T> d = load_unit(g + k, H - k);
+            Unit<T> u[S];
+#pragma unroll
+            for (int q = 0; q < S; ++q)
+                if (has[q]) u[q] = load_unit(rows + at[q] * stride + k, H - k);
+#pragma unroll
+            for (int q = 0; q < S; ++q)
+                if (has[q]) {
+                    Unit<T> o;
+#pragma unroll
+                    for (int c = 0; c < UNIT<T>; ++c) {
+                        const float v = to_float(d.v[c]);
+                        dot[q] = fmaf(v, to_float(u[q].v[c]), dot[q]);
+                        o.v[c] = (T)(w[q] * v);
+                    }
+                    store_unit(drows + at[q] * drows_stride + k, H - k, o);
+                }
+        }
+#pragma unroll
+        for (int q = 0; q < S; ++q) dot[q] = group_reduce<(L < 64 ? L : 64)>(dot[q], Plus{});
+        if constexpr (L == 256) {
+            __shared__ float part[4][S];
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+                for (int q = 0; q < S; ++q) part[threadIdx.x >> 6][q] = dot[q];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int q = 0; q < S; ++q) dot[q] = (part[0][q] + part[1][q]) + (part[2][q] + part[3][q]);
+        }
+        if (j == 0) {
+#pragma unroll
+            for (int q = 0; q < S; ++q)
+                if (s0 + q < top) dweights[n * top + s0 + q] = dot[q];
+        }
     }
 }
 
-unsigned blocks_for(int64_t work, int64_t per, int64_t most) {
-    const int64_t b = (work + per - 1) / per;
-    return (unsigned)(b < most ? b : most);
+// f(integral_constant<L>, integral_constant<UN>) for rows of `units` units
+template <class F>
+void row_lanes(int64_t units, F&& f) {
+#define EINET_L(LL, UU) f(std::integral_constant<int, LL>{}, std::integral_constant<int, UU>{})
+    if (units <= 1) EINET_L(1, 1);
+    else if (units <= 2) EINET_L(2, 1);
+    else if (units <= 4) EINET_L(4, 1);
+    else if (units <= 8) EINET_L(8, 1);
+    else if (units <= 16) EINET_L(16, 1);
+    else if (units <= 32) EINET_L(32, 1);
+    else if (units <= 64) EINET_L(64, 1);
+    else if (units <= 128) EINET_L(64, 2);
+    else EINET_L(64, 4);
+#undef EINET_L
 }
 
 }  // namespace
 
+// f(T{}, K{}) for the types of the scores and of their sums with the coefficients
+template <class F>
+void route_types(const Scores& a, F&& f) {
+    with_type(a.type, [&](auto t) {
+        if (a.coef) f(t, double{});
+        else f(t, float{});
+    });
+}
+
 void launch_route(const Scores& a, int top, bool renormalise, int32_t* ids, float* weights, float* logp, hipStream_t s) {
     if (a.N == 0) return;
-    with_type(a.type, [&](auto t) {
+    const int re = renormalise ? 1 : 0;
+    route_types(a, [&](auto t, auto k) {
         using T = decltype(t);
+        using K = decltype(k);
+        const T* const p = static_cast<const T*>(a.p);
+        if (route_by_columns(a, top)) {
+            const dim3 grid((unsigned)((a.N + 255) / 256));
+            if (top == 1) hipLaunchKernelGGL((k_route_columns<T, K, 1>), grid, dim3(256), 0, s, p, a.sc, a.coef, a.M, a.N, top, re, ids, weights, logp);
+            else if (top == 2) hipLaunchKernelGGL((k_route_columns<T, K, 2>), grid, dim3(256), 0, s, p, a.sc, a.coef, a.M, a.N, top, re, ids, weights, logp);
+            else hipLaunchKernelGGL((k_route_columns<T, K, 4>), grid, dim3(256), 0, s, p, a.sc, a.coef, a.M, a.N, top, re, ids, weights, logp);
+            return;
+        }
         route_variant(a.M, top, [&](auto g, auto e) {
             constexpr int G = decltype(g)::value, E = decltype(e)::value;
-            hipLaunchKernelGGL((k_route<T, G, E>), dim3((unsigned)((a.N + 256 / G - 1) / (256 / G))), dim3(256), 0, s,
-                               static_cast<const T*>(a.p), a.sc, a.sn, a.coef, a.M, a.N, top, renormalise ? 1 : 0, ids, weights,
-                               logp);
+            hipLaunchKernelGGL((k_route<T, K, G, E>), dim3((unsigned)((a.N + 256 / G - 1) / (256 / G))), dim3(256), 0, s, p, a.sc,
+                               a.sn, a.coef, a.M, a.N, top, re, ids, weights, logp);
         });
     });
 }
 
-size_t route_backward_workspace(int M, int64_t N) { return sizeof(float) * (size_t)route_backward_groups(M, N) * M; }
+size_t route_backward_workspace(int M, int64_t N) { return sizeof(float) * (size_t)route_backward_groups(N) * M; }
 
 void launch_route_backward(const Scores& a, int top, bool renormalise, const int32_t* ids, const float* weights,
                            const float* dweights, const float* dlogp, void* dscores, int64_t dsc, int64_t dsn, float* dcoef,
                            void* workspace, hipStream_t s) {
-    const int groups = route_backward_groups(a.M, a.N);
+    const int groups = route_backward_groups(a.N), re = renormalise ? 1 : 0;
     float* const partial = dcoef ? static_cast<float*>(workspace) : nullptr;
     if (a.N > 0)
-        with_type(a.type, [&](auto t) {
+        route_types(a, [&](auto t, auto k) {
             using T = decltype(t);
+            using K = decltype(k);
+            const T* const p = static_cast<const T*>(a.p);
+            T* const d = static_cast<T*>(dscores);
+            if (route_by_columns(a, top) && dsn == 1) {
+                hipLaunchKernelGGL((k_route_backward_columns<T, K>), dim3(groups), dim3(256), 0, s, p, a.sc, a.coef, a.M, a.N, top,
+                                   re, ids, weights, dweights, dlogp, d, dsc, partial);
+                return;
+            }
             route_variant(a.M, top, [&](auto g, auto e) {
                 constexpr int G = decltype(g)::value, E = decltype(e)::value;
-                hipLaunchKernelGGL((k_route_backward<T, G, E>), dim3(groups), dim3(256), 0, s, static_cast<const T*>(a.p), a.sc,
-                                   a.sn, a.coef, a.M, a.N, top, renormalise ? 1 : 0, ids, weights, dweights, dlogp,
-                                   static_cast<T*>(dscores), dsc, dsn, partial);
+                hipLaunchKernelGGL((k_route_backward<T, K, G, E>), dim3(groups), dim3(256), 0, s, p, a.sc, a.sn, a.coef, a.M, a.N,
+                                   top, re, ids, weights, dweights, dlogp, d, dsc, dsn, partial);
             });
         });
-    if (dcoef) hipLaunchKernelGGL(k_route_coef, dim3((a.M + 63) / 64), dim3(256), 0, s, partial, groups, a.M, dcoef);
+    if (dcoef) hipLaunchKernelGGL(k_route_coef, dim3((a.M + 31) / 32), dim3(1024), 0, s, partial, groups, a.M, dcoef);
 }
 
-size_t sort_workspace(int64_t, int) { return 0; }
+size_t sort_workspace(int64_t slots, int M) {
+    const int blocks = sort_blocks(slots);
+    return blocks > 1 ? sizeof(int32_t) * (size_t)blocks * M : 0;
+}
 
-void launch_sort(const int32_t* ids, int64_t slots, int M, int32_t* first, int32_t* place, void*, hipStream_t s) {
+void launch_sort(const int32_t* ids, int64_t slots, int M, int32_t* first, int32_t* place, void* workspace, hipStream_t s) {
     int bits = 1;
     while ((1 << bits) <= M) ++bits;
+    const int blocks = sort_blocks(slots);
+    int32_t* const counts = static_cast<int32_t*>(workspace);
+    if (blocks > 1) hipLaunchKernelGGL(k_sort_count, dim3(blocks), dim3(64 * SORT_WAVES), 0, s, ids, slots, M, counts);
     const size_t lds = sizeof(int32_t) * (size_t)(SORT_WAVES * M + SORT_WAVES);
-    allow_dynamic_lds(k_sort, lds);
-    hipLaunchKernelGGL(k_sort, dim3(1), dim3(64 * SORT_WAVES), lds, s, ids, slots, M, bits, first, place);
+    if (lds > 65536) allow_dynamic_lds(k_sort, lds);
+    hipLaunchKernelGGL(k_sort, dim3(blocks), dim3(64 * SORT_WAVES), lds, s, ids, slots, M, bits, counts, first, place);
+}
+
+// Rows are split into launches of fewer than 2^32 items, and of fewer than 2^31 workgroups: f(first sample, samples).
+template <class F>
+void row_batches(int64_t N, int64_t tiles, F&& f) {
+    const int64_t most = (int64_t)0x7fffffff / tiles > 0 ? (int64_t)0x7fffffff / tiles : 1;
+    for (int64_t n0 = 0; n0 < N; n0 += most) f(n0, N - n0 < most ? N - n0 : most);
 }
 
 void launch_dispatch(const void* x, int64_t row_bytes, int64_t x_stride, int64_t N, int top, const int32_t* place, void* out,
                      int64_t out_stride, int64_t out_rows, hipStream_t s) {
-    if (N == 0 || row_bytes == 0) return;
+    if (N == 0 || row_bytes == 0 || out_rows == 0) return;
     const uint64_t any = (uint64_t)row_bytes | (uint64_t)x_stride | (uint64_t)out_stride | reinterpret_cast<uintptr_t>(x) |
                          reinterpret_cast<uintptr_t>(out);
-    auto go = [&](auto u) {
-        using U = decltype(u);
-        const int64_t units = row_bytes / (int64_t)sizeof(U);
-        hipLaunchKernelGGL(k_dispatch<U>, dim3(blocks_for(N * units, 256, 16384)), dim3(256), 0, s, static_cast<const char*>(x),
-                           units, x_stride, N, top, place, static_cast<char*>(out), out_stride, out_rows);
+    auto go = [&](auto t) {
+        using T = decltype(t);
+        constexpr int64_t e = sizeof(T);
+        const int64_t H = row_bytes / e, units = (H + UNIT<T> - 1) / UNIT<T>;
+        row_lanes(units, [&](auto l, auto un) {
+            constexpr int L = decltype(l)::value, UN = decltype(un)::value;
+            const int64_t tiles = (units + L * UN - 1) / (L * UN);
+            row_batches(N, tiles, [&](int64_t n0, int64_t n) {
+                hipLaunchKernelGGL((k_dispatch<T, L, UN>), dim3((unsigned)((n * tiles + 256 / L - 1) / (256 / L))), dim3(256), 0, s,
+                                   static_cast<const T*>(x) + n0 * (x_stride / e), H, x_stride / e, n, (int)tiles, top,
+                                   place + n0 * top, static_cast<T*>(out), out_stride / e, out_rows);
+            });
+        });
     };
-    if (any % 16 == 0) go(uint4{});
-    else if (any % 4 == 0) go(uint32_t{});
+    if (any % 4 == 0) go(uint32_t{});
     else if (any % 2 == 0) go(uint16_t{});
     else go(uint8_t{});
 }
@@ -424,8 +862,22 @@ void launch_combine(const void* rows, int type, int64_t H, int64_t stride, int64
     if (N == 0 || H == 0) return;
     with_type(type, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL(k_combine<T>, dim3(blocks_for(N * H, 256, 16384)), dim3(256), 0, s, static_cast<const T*>(rows), H,
-                           stride, n_rows, place, weights, N, top, static_cast<T*>(out), out_stride);
+        const int64_t units = (H + UNIT<T> - 1) / UNIT<T>;
+        row_lanes(units, [&](auto l, auto un) {
+            constexpr int L = decltype(l)::value, UN = decltype(un)::value;
+            const int64_t tiles = (units + L * UN - 1) / (L * UN);
+            row_batches(N, tiles, [&](int64_t n0, int64_t n) {
+                const dim3 grid((unsigned)((n * tiles + 256 / L - 1) / (256 / L)));
+                const T* const r = static_cast<const T*>(rows);
+                T* const o = static_cast<T*>(out) + n0 * out_stride;
+                const int32_t* const at = place + n0 * top;
+                const float* const w = weights ? weights + n0 * top : nullptr;
+                if (top == 1)
+                    hipLaunchKernelGGL((k_combine<T, L, UN, 1>), grid, dim3(256), 0, s, r, H, stride, n_rows, at, w, n, (int)tiles, top, o, out_stride);
+                else
+                    hipLaunchKernelGGL((k_combine<T, L, UN, 2>), grid, dim3(256), 0, s, r, H, stride, n_rows, at, w, n, (int)tiles, top, o, out_stride);
+            });
+        });
     });
 }
 
@@ -435,9 +887,23 @@ void launch_combine_backward(const void* dout, int64_t dout_stride, const void* 
     if (N == 0) return;
     with_type(type, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL(k_combine_backward<T>, dim3(blocks_for(N * top, 4, 16384)), dim3(256), 0, s,
-                           static_cast<const T*>(dout), dout_stride, static_cast<const T*>(rows), H, stride, n_rows, place,
-                           weights, N * top, top, static_cast<T*>(drows), drows_stride, dweights);
+        const int64_t units = (H + UNIT<T> - 1) / UNIT<T>;
+        auto go = [&](auto l) {
+            constexpr int L = decltype(l)::value;
+            const dim3 grid((unsigned)((N + 256 / L - 1) / (256 / L)));
+            const T* const g = static_cast<const T*>(dout);
+            const T* const r = static_cast<const T*>(rows);
+            T* const d = static_cast<T*>(drows);
+            if (top == 1)
+                hipLaunchKernelGGL((k_combine_backward<T, L, 1>), grid, dim3(256), 0, s, g, dout_stride, r, H, stride, n_rows, place, weights, N, top, d, drows_stride, dweights);
+            else if (top == 2)
+                hipLaunchKernelGGL((k_combine_backward<T, L, 2>), grid, dim3(256), 0, s, g, dout_stride, r, H, stride, n_rows, place, weights, N, top, d, drows_stride, dweights);
+            else
+                hipLaunchKernelGGL((k_combine_backward<T, L, 4>), grid, dim3(256), 0, s, g, dout_stride, r, H, stride, n_rows, place, weights, N, top, d, drows_stride, dweights);
+        };
+        // (few samples with long rows: a workgroup each instead of a wave)
+        if (units > 64 && N < 8 * EINET_NUM_CUS) go(std::integral_constant<int, 256>{});
+        else row_lanes(units, [&](auto l, auto) { go(l); });
     });
 }
 
