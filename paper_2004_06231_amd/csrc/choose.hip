@@ -113,6 +113,9 @@ __device__ __forceinline__ u64 target_of(double u, u64 total) {
     return t >= (double)total ? total - 1 : min((u64)t, total - 1);
 }
 
+// the mass that the entries kept by top_p reach, 1 .. total
+__device__ __forceinline__ u64 mass_of(double top_p, u64 total) { return max((u64)1, __double2ull_ru(top_p * (double)total)); }
+
 // N consecutive entries of a row, of which the first `count` exist; the hardware loads them at any alignment at once
 template <class T, int N>
 __device__ __forceinline__ void load_keys(const T* x, int count, uint32_t (&k)[N]) {
@@ -257,7 +260,7 @@ __global__ __launch_bounds__(256) void k_choose_wave(ChooseArgs a, int shift) {
         }
     }
     if (st.top_p < 1.0) {
-        const u64 total = mass_from(1), mass = max((u64)1, __double2ull_ru(st.top_p * (double)total));
+        const u64 mass = mass_of(st.top_p, mass_from(1));
         uint32_t lo = 1, hi = kmax + 1;                          // at least `mass` from lo on, less from hi on
         int n_lo = count_from(1), n_hi = 0;
         u64 m_hi = 0;
@@ -332,7 +335,8 @@ struct RowKeys {
     const T* x;
     int V, first, groups;        // of this thread's wave: its first group, the number of its groups
     uint32_t k[GROUPS > 0 ? GROUPS * 4 : 1];
-    __device__ void init(const T* row, int n) {
+    // entries 0 .. n-1 of row; another origin only moves the indexes that the caller adds
+    __device__ __forceinline__ void init(const T* row, int n) {
         x = row;
         V = n;
         const int wave = threadIdx.x >> 6;
@@ -352,10 +356,11 @@ struct RowKeys {
             first = wave * groups;
         }
     }
+    __device__ __forceinline__ int index(int g) const { return (first + g) * 256 + (int)(threadIdx.x & 63) * 4; }
     // f(index, key) for the four entries of a group
     template <class F>
     __device__ __forceinline__ void group(int g, F&& f) const {
-        const int i0 = (first + g) * 256 + (int)(threadIdx.x & 63) * 4;
+        const int i0 = index(g);
         uint32_t part[4];
         load_keys<T, 4>(x + i0, V - i0, part);
 #pragma unroll
@@ -367,12 +372,24 @@ struct RowKeys {
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) f((first + g) * 256 + (int)(threadIdx.x & 63) * 4 + c, k[g * 4 + c]);
+                for (int c = 0; c < 4; ++c) f(index(g) + c, k[g * 4 + c]);
         } else {
-            for (int g = 0; g < groups; ++g) group(g, f);
+            int g = 0;
+            for (; g + 4 <= groups; g += 4) {                    // (four loads in flight)
+                uint32_t part[4][4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) load_keys<T, 4>(x + index(g + q), V - index(g + q), part[q]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) f(index(g + q) + c, part[q][c]);
+            }
+            for (; g < groups; ++g) group(g, f);
         }
     }
 };
+
+constexpr float BIN_RANGE = 32.f;       // in units of T: a weight beyond is below 2e-14 of the largest
 
 template <int NT>
 struct ChooseShared {
@@ -465,91 +482,26 @@ __device__ __forceinline__ u64 find_entry(Each&& each, u64 target, ChooseShared<
     return prefix;
 }
 
-template <class T, int NT, int GROUPS>
-__global__ __launch_bounds__(NT) void k_choose_block(ChooseArgs a, int shift) {
-    __shared__ ChooseShared<NT> sh;
-    constexpr int BINS = ChooseShared<NT>::BINS;
-    const int row = blockIdx.x, tid = threadIdx.x, V = a.V;
-    const RowSettings st = row_settings(a, row);
-    RowKeys<T, NT, GROUPS> keys;
-    keys.init(static_cast<const T*>(a.logits) + row * a.stride, V);
-    u64 best = 0;
-    keys.each([&](int i, uint32_t k) { best = max(best, k ? order_key(k, i) : 0); });
-    best = block_reduce<NT>(best, sh.tmp, OpMax{});
-    const uint32_t kmax = (uint32_t)(best >> 32);
-    if (kmax == 0u || st.greedy) {
-        if (tid == 0) {
-            a.index[row] = kmax ? (int)~(uint32_t)best : -1;
-            if (a.logq) a.logq[row] = kmax ? 0.f : -INFINITY;
-        }
-        return;
-    }
-    const RowWeights<T> weight{kmax, key_logit<T>(kmax), st.log2e_t, shift};
-    const float per_bin = st.inv_t * (float)(BINS / 32);
-    auto bin_of = [&](uint32_t k) {
-        const float q = (weight.m - key_logit<T>(k)) * per_bin;
-        return k == kmax ? 0 : q < (float)(BINS - 1) ? (int)q : BINS - 1;
-    };
-    u64 cut = 1ull << 32;                                        // everything that is not left out
-    const bool by_count = st.top_k > 0 && st.top_k < V, by_mass = st.top_p < 1.0;
-    if (by_count || by_mass) {
-        for (int b = tid; b < BINS; b += NT) sh.count[b] = 0, sh.mass[b] = 0;
-        __syncthreads();
-        keys.each([&](int, uint32_t k) {
-            if (k == 0u) return;
-            const int b = bin_of(k);
-            if (by_count) atomicAdd(&sh.count[b], 1u);
-            if (by_mass) atomicAdd(&sh.mass[b], weight(k));
-        });
-        __syncthreads();
-        // entries of a bin from the cut on, with their values
-        auto of_bin = [&](int bin, auto value) {
-            return [&, bin, value](auto f) {
-                keys.each([&](int i, uint32_t k) {
-                    if (k == 0u || bin_of(k) != bin) return;
-                    const u64 o = order_key(k, i);
-                    if (o >= cut) f(o, value(k));
-                });
-            };
-        };
-        int bin;
-        u64 missing, total;
-        if (by_count) {
-            block_scan<NT>((u64)sh.count[2 * tid] + sh.count[2 * tid + 1], sh.tmp, total);
-            if (total > (u64)st.top_k) {
-                find_bin<NT>(sh.count, (u64)st.top_k, sh, bin, missing);
-                cut = find_entry<NT>(of_bin(bin, [](uint32_t) -> u64 { return 1; }), missing, sh);
-                if (by_mass) {
-                    // the mass of that bin is what is kept of it, that of the bins behind it none
-                    u64 rest = 0;
-                    of_bin(bin, weight)([&](u64, u64 v) { rest += v; });
-                    rest = block_reduce<NT>(rest, sh.tmp, OpAdd{});
-                    for (int b = tid; b < BINS; b += NT)
-                        if (b >= bin) sh.mass[b] = b == bin ? rest : 0;
-                    __syncthreads();
-                }
-            }
-        }
-        if (by_mass) {
-            block_scan<NT>(sh.mass[2 * tid] + sh.mass[2 * tid + 1], sh.tmp, total);
-            // kept: what has less than top_p of the total before it; the last one's own weight reaches that mass
-            find_bin<NT>(sh.mass, max((u64)1, __double2ull_ru(st.top_p * (double)total)), sh, bin, missing);
-            cut = find_entry<NT>(of_bin(bin, weight), missing, sh);
-        }
-    }
-    const u64 least = weight.least(st.min_p);
-    auto kept = [&](int i, uint32_t k) {
-        if (k == 0u || order_key(k, i) < cut) return (u64)0;
-        const u64 w = weight(k);
-        return w < least ? (u64)0 : w;
-    };
-    u64 mine = 0, total;
-    keys.each([&](int i, uint32_t k) { mine += kept(i, k); });
-    const u64 wave_sum = wave_reduce(mine, OpAdd{});
-    const u64 end = block_scan<NT>((tid & 63) == 63 ? wave_sum : 0, sh.tmp, total);
-    const u64 target = target_of(st.u, total);
-    // the wave in whose stretch the running sum exceeds the target goes through its groups
-    u64 run = lane_value(end, 63) - wave_sum;
+// The bin of a key: its distance from the largest logit, per_bin = bins / (BIN_RANGE T).
+template <class T>
+__device__ __forceinline__ int bin_of(const RowWeights<T>& weight, uint32_t k, float per_bin, int bins) {
+    const float q = (weight.m - key_logit<T>(k)) * per_bin;
+    return k == weight.kmax ? 0 : q < (float)(bins - 1) ? (int)q : bins - 1;
+}
+
+__device__ __forceinline__ void write_choice(const ChooseArgs& a, int row, int index, float logq) {
+    a.index[row] = index;
+    if (a.logq) a.logq[row] = logq;
+}
+
+// The choice among the entries of `keys` (those of the row from `origin` on), of which kept(index, key) is the kept weight:
+// the first at which the running sum, `before` at the start, exceeds target.  total: of all kept weights of the row.
+template <class T, int NT, int GROUPS, class Kept>
+__device__ __forceinline__ void choose_among(const ChooseArgs& a, int row, const RowKeys<T, NT, GROUPS>& keys, int origin, u64 before,
+                                             u64 target, u64 total, u64 wave_sum, u64 wave_end, const RowWeights<T>& weight,
+                                             Kept&& kept) {
+    // the wave in whose stretch that is goes through its groups
+    u64 run = before + wave_end - wave_sum;
     if (target < run || target >= run + wave_sum) return;
     for (int g = 0; g < keys.groups; ++g) {
         u64 w[4], sum = 0;
@@ -564,16 +516,16 @@ __global__ __launch_bounds__(NT) void k_choose_block(ChooseArgs a, int shift) {
         const u64 ends = wave_scan(sum, OpAdd{}) + run;
         const u64 above = __ballot(ends > target);
         if (above) {
-            if ((tid & 63) == __ffsll(above) - 1) {
+            if ((int)(threadIdx.x & 63) == __ffsll(above) - 1) {
                 u64 s = ends;
                 int at = 3;
 #pragma unroll
-                for (int c = 3; c > 0; --c) {
-                    s -= w[c];
-                    if (s > target) at = c - 1;
+                for (int q = 3; q > 0; --q) {
+                    s -= w[q];                                   // the running sum at place q - 1
+                    if (s > target) at = q - 1;
                 }
-                a.index[row] = (keys.first + g) * 256 + (tid & 63) * 4 + at;
-                if (a.logq) a.logq[row] = weight.log_share(at == 0 ? k4[0] : at == 1 ? k4[1] : at == 2 ? k4[2] : k4[3], total);
+                const uint32_t key = at == 0 ? k4[0] : at == 1 ? k4[1] : at == 2 ? k4[2] : k4[3];
+                write_choice(a, row, origin + keys.index(g) + at, weight.log_share(key, total));
             }
             return;
         }
@@ -581,10 +533,375 @@ __global__ __launch_bounds__(NT) void k_choose_block(ChooseArgs a, int shift) {
     }
 }
 
+template <class T, int NT, int GROUPS>
+__device__ __forceinline__ void choose_block(const ChooseArgs& a, int row, int shift, ChooseShared<NT>& sh) {
+    constexpr int BINS = ChooseShared<NT>::BINS;
+    const int tid = threadIdx.x, V = a.V;
+    const RowSettings st = row_settings(a, row);
+    RowKeys<T, NT, GROUPS> keys;
+    keys.init(static_cast<const T*>(a.logits) + row * a.stride, V);
+    u64 best = 0;
+    keys.each([&](int i, uint32_t k) { best = max(best, k ? order_key(k, i) : 0); });
+    best = block_reduce<NT>(best, sh.tmp, OpMax{});
+    const uint32_t kmax = (uint32_t)(best >> 32);
+    if (kmax == 0u || st.greedy) {
+        if (tid == 0) write_choice(a, row, kmax ? (int)~(uint32_t)best : -1, kmax ? 0.f : -INFINITY);
+        return;
+    }
+    const RowWeights<T> weight{kmax, key_logit<T>(kmax), st.log2e_t, shift};
+    const float per_bin = st.inv_t * ((float)BINS / BIN_RANGE);
+    auto bin = [&](uint32_t k) { return bin_of(weight, k, per_bin, BINS); };
+    u64 cut = 1ull << 32;                                        // everything that is not left out
+    const bool by_count = st.top_k > 0 && st.top_k < V, by_mass = st.top_p < 1.0;
+    if (by_count || by_mass) {
+        for (int b = tid; b < BINS; b += NT) sh.count[b] = 0, sh.mass[b] = 0;
+        __syncthreads();
+        keys.each([&](int, uint32_t k) {
+            if (k == 0u) return;
+            const int b = bin(k);
+            if (by_count) atomicAdd(&sh.count[b], 1u);
+            if (by_mass) atomicAdd(&sh.mass[b], weight(k));
+        });
+        __syncthreads();
+        // entries of a bin from the cut on, with their values
+        auto of_bin = [&](int at, auto value) {
+            return [&, at, value](auto f) {
+                keys.each([&](int i, uint32_t k) {
+                    if (k == 0u || bin(k) != at) return;
+                    const u64 o = order_key(k, i);
+                    if (o >= cut) f(o, value(k));
+                });
+            };
+        };
+        int at;
+        u64 missing, total;
+        if (by_count) {
+            block_scan<NT>((u64)sh.count[2 * tid] + sh.count[2 * tid + 1], sh.tmp, total);
+            if (total > (u64)st.top_k) {
+                find_bin<NT>(sh.count, (u64)st.top_k, sh, at, missing);
+                cut = find_entry<NT>(of_bin(at, [](uint32_t) -> u64 { return 1; }), missing, sh);
+                if (by_mass) {
+                    // the mass of that bin is what is kept of it, that of the bins behind it none
+                    u64 rest = 0;
+                    of_bin(at, weight)([&](u64, u64 v) { rest += v; });
+                    rest = block_reduce<NT>(rest, sh.tmp, OpAdd{});
+                    for (int b = tid; b < BINS; b += NT)
+                        if (b >= at) sh.mass[b] = b == at ? rest : 0;
+                    __syncthreads();
+                }
+            }
+        }
+        if (by_mass) {
+            block_scan<NT>(sh.mass[2 * tid] + sh.mass[2 * tid + 1], sh.tmp, total);
+            // kept: what has less than top_p of the total before it; the last one's own weight reaches that mass
+            find_bin<NT>(sh.mass, mass_of(st.top_p, total), sh, at, missing);
+            cut = find_entry<NT>(of_bin(at, weight), missing, sh);
+        }
+    }
+    const u64 least = weight.least(st.min_p);
+    auto kept = [&](int i, uint32_t k) {
+        if (k == 0u || order_key(k, i) < cut) return (u64)0;
+        const u64 w = weight(k);
+        return w < least ? (u64)0 : w;
+    };
+    u64 mine = 0, total;
+    keys.each([&](int i, uint32_t k) { mine += kept(i, k); });
+    const u64 wave_sum = wave_reduce(mine, OpAdd{});
+    const u64 end = lane_value(block_scan<NT>((tid & 63) == 63 ? wave_sum : 0, sh.tmp, total), 63);
+    choose_among(a, row, keys, 0, 0, target_of(st.u, total), total, wave_sum, end, weight, kept);
+}
+
+template <class T, int NT, int GROUPS>
+__global__ __launch_bounds__(NT) void k_choose_block(ChooseArgs a, int shift) {
+    __shared__ ChooseShared<NT> sh;
+    choose_block<T, NT, GROUPS>(a, blockIdx.x, shift, sh);
+}
+
+// ------------------------------------------------------------------------------------ several workgroups for every row
+//
+// Few long rows: `parts` workgroups of SPLIT_THREADS for every row, each with a stretch of `per` entries, in four launches
+// (three where no filter is on).
+//   max      the largest order key of every part
+//   bins     the row's histogram over the distance from the largest logit, summed up by integer atomics (exact, in any
+//            order); rows without top_k and top_p: the kept mass of every part instead
+//   collect  the bin that the cut lies in, from the row's histogram.  With top_k: all entries up to that bin go to a list,
+//            at most LIST of them.  With top_p alone: that bin's entries do, and every part's kept mass in the bins before it
+//            is written down.
+//   finish   one workgroup per row finds the cut among the list's entries, the choice among them (top_k) or in the part in
+//            which the running sum exceeds the target.  A row whose list did not hold its entries (more than LIST entries
+//            nearly as large as each other) and one with top_k above LIST are done as a workgroup for every row does it.
+constexpr int SPLIT_THREADS = 256, SPLIT_BINS = 2 * SPLIT_THREADS, LIST = 4096, FINISH_THREADS = 1024;
+constexpr int SPLIT_PARTS = 64;                                  // at most (a lane each)
+
+struct SplitRows {
+    int parts, per;
+    u64* best;                   // [B][parts]
+    u64* mass;                   // [B][parts]
+    u64* bin_mass;               // [B][SPLIT_BINS]
+    uint32_t* bin_count;         // [B][SPLIT_BINS]
+    uint32_t* listed;            // [B] entries of the list, also those that it did not hold
+    u64* list;                   // [B][LIST] order keys
+};
+
+enum SplitMode { SPLIT_NONE, SPLIT_ALL, SPLIT_COUNT, SPLIT_MASS, SPLIT_BLOCK };
+
+// What a row's workgroups agree on from its settings and the largest keys of its parts.
+template <class T>
+struct SplitRow {
+    RowSettings st;
+    u64 best;
+    bool done;                   // no entry, or the largest one
+    RowWeights<T> weight;
+    float per_bin;
+    __device__ __forceinline__ SplitRow(const ChooseArgs& a, const SplitRows& sp, int row, int shift) {
+        st = row_settings(a, row);
+        const int lane = threadIdx.x & 63;
+        best = wave_reduce(lane < sp.parts ? sp.best[(size_t)row * sp.parts + lane] : 0, OpMax{});
+        const uint32_t kmax = (uint32_t)(best >> 32);
+        done = kmax == 0u || st.greedy;
+        weight = RowWeights<T>{kmax, key_logit<T>(kmax), st.log2e_t, shift};
+        per_bin = st.inv_t * ((float)SPLIT_BINS / BIN_RANGE);
+    }
+    __device__ __forceinline__ bool by_count(int V) const { return st.top_k > 0 && st.top_k < V; }
+    __device__ __forceinline__ bool by_mass() const { return st.top_p < 1.0; }
+    __device__ __forceinline__ int bin(uint32_t k) const { return bin_of(weight, k, per_bin, SPLIT_BINS); }
+};
+
+// the part's entries as RowKeys; index 0 of them is entry `origin` of the row
+template <class T>
+__device__ __forceinline__ int split_part(const ChooseArgs& a, const SplitRows& sp, int row, int part, RowKeys<T, SPLIT_THREADS, 0>& keys) {
+    const int origin = part * sp.per;
+    keys.init(static_cast<const T*>(a.logits) + row * a.stride + origin, min(sp.per, a.V - origin));
+    return origin;
+}
+
+template <class T>
+__global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_max(ChooseArgs a, SplitRows sp) {
+    __shared__ u64 tmp[SPLIT_THREADS / 64];
+    const int row = blockIdx.x / sp.parts, part = blockIdx.x - row * sp.parts, tid = threadIdx.x;
+    for (int b = part * SPLIT_THREADS + tid; b < SPLIT_BINS; b += sp.parts * SPLIT_THREADS) {
+        sp.bin_count[(size_t)row * SPLIT_BINS + b] = 0;
+        sp.bin_mass[(size_t)row * SPLIT_BINS + b] = 0;
+    }
+    if (part == 0 && tid == 0) sp.listed[row] = 0;
+    RowKeys<T, SPLIT_THREADS, 0> keys;
+    const int origin = split_part(a, sp, row, part, keys);
+    u64 best = 0;
+    keys.each([&](int i, uint32_t k) { best = max(best, k ? order_key(k, origin + i) : 0); });
+    best = block_reduce<SPLIT_THREADS>(best, tmp, OpMax{});
+    if (tid == 0) sp.best[(size_t)row * sp.parts + part] = best;
+}
+
+template <class T>
+__global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_bins(ChooseArgs a, SplitRows sp, int shift) {
+    __shared__ u64 mass[SPLIT_BINS], tmp[SPLIT_THREADS / 64];
+    __shared__ uint32_t count[SPLIT_BINS];
+    const int row = blockIdx.x / sp.parts, part = blockIdx.x - row * sp.parts, tid = threadIdx.x;
+    const SplitRow<T> r(a, sp, row, shift);
+    if (r.done) return;
+    RowKeys<T, SPLIT_THREADS, 0> keys;
+    split_part(a, sp, row, part, keys);
+    const bool by_count = r.by_count(a.V), by_mass = r.by_mass();
+    if (!by_count && !by_mass) {
+        const u64 least = r.weight.least(r.st.min_p);
+        u64 sum = 0;
+        keys.each([&](int, uint32_t k) {
+            const u64 w = r.weight(k);
+            sum += w < least ? 0 : w;
+        });
+        sum = block_reduce<SPLIT_THREADS>(sum, tmp, OpAdd{});
+        if (tid == 0) sp.mass[(size_t)row * sp.parts + part] = sum;
+        return;
+    }
+    for (int b = tid; b < SPLIT_BINS; b += SPLIT_THREADS) count[b] = 0, mass[b] = 0;
+    __syncthreads();
+    // (with top_k the masses are those of the list's entries)
+    keys.each([&](int, uint32_t k) {
+        if (k == 0u) return;
+        const int b = r.bin(k);
+        if (by_count) atomicAdd(&count[b], 1u);
+        else atomicAdd(&mass[b], r.weight(k));
+    });
+    __syncthreads();
+    for (int b = tid; b < SPLIT_BINS; b += SPLIT_THREADS) {
+        if (count[b]) atomicAdd(&sp.bin_count[(size_t)row * SPLIT_BINS + b], count[b]);
+        if (mass[b]) atomicAdd(&sp.bin_mass[(size_t)row * SPLIT_BINS + b], mass[b]);
+    }
+}
+
+// The row's mode and the bin that its cut lies in; missing: what is to be reached within that bin (top_p alone).
+template <class T>
+__device__ __forceinline__ SplitMode split_cut_bin(const ChooseArgs& a, const SplitRows& sp, const SplitRow<T>& r, int row,
+                                                   ChooseShared<SPLIT_THREADS>& sh, int& bin, u64& missing) {
+    const int tid = threadIdx.x, b = 2 * tid;
+    if (r.done) return SPLIT_NONE;
+    if (!r.by_count(a.V) && !r.by_mass()) return SPLIT_ALL;
+    u64 total;
+    if (r.by_count(a.V)) {
+        sh.count[b] = sp.bin_count[(size_t)row * SPLIT_BINS + b];
+        sh.count[b + 1] = sp.bin_count[(size_t)row * SPLIT_BINS + b + 1];
+        block_scan<SPLIT_THREADS>((u64)sh.count[b] + sh.count[b + 1], sh.tmp, total);
+        if (r.st.top_k > LIST) return SPLIT_BLOCK;
+        find_bin<SPLIT_THREADS>(sh.count, min((u64)r.st.top_k, total), sh, bin, missing);
+        return SPLIT_COUNT;
+    }
+    sh.mass[b] = sp.bin_mass[(size_t)row * SPLIT_BINS + b];
+    sh.mass[b + 1] = sp.bin_mass[(size_t)row * SPLIT_BINS + b + 1];
+    block_scan<SPLIT_THREADS>(sh.mass[b] + sh.mass[b + 1], sh.tmp, total);
+    find_bin<SPLIT_THREADS>(sh.mass, mass_of(r.st.top_p, total), sh, bin, missing);
+    return SPLIT_MASS;
+}
+
+template <class T>
+__global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_collect(ChooseArgs a, SplitRows sp, int shift) {
+    __shared__ ChooseShared<SPLIT_THREADS> sh;
+    const int row = blockIdx.x / sp.parts, part = blockIdx.x - row * sp.parts, tid = threadIdx.x, lane = tid & 63;
+    const SplitRow<T> r(a, sp, row, shift);
+    int bin;
+    u64 missing;
+    const SplitMode mode = split_cut_bin(a, sp, r, row, sh, bin, missing);
+    if (mode != SPLIT_COUNT && mode != SPLIT_MASS) return;
+    RowKeys<T, SPLIT_THREADS, 0> keys;
+    const int origin = split_part(a, sp, row, part, keys);
+    const u64 least = r.weight.least(r.st.min_p);
+    u64 sum = 0;
+    keys.each([&](int i, uint32_t k) {
+        const int b = k ? r.bin(k) : SPLIT_BINS;
+        const bool take = mode == SPLIT_COUNT ? b <= bin : b == bin;
+        if (mode == SPLIT_MASS && b < bin) {
+            const u64 w = r.weight(k);
+            sum += w < least ? 0 : w;
+        }
+        const u64 takers = __ballot(take);
+        if (!takers) return;
+        uint32_t at = 0;
+        if (lane == __ffsll(takers) - 1) at = atomicAdd(&sp.listed[row], (uint32_t)__popcll(takers));
+        at = (uint32_t)__builtin_amdgcn_readlane((int)at, __ffsll(takers) - 1) + __popcll(takers & ((1ull << lane) - 1));
+        if (take && at < LIST) sp.list[(size_t)row * LIST + at] = order_key(k, origin + i);
+    });
+    if (mode == SPLIT_MASS) {
+        sum = block_reduce<SPLIT_THREADS>(sum, sh.tmp, OpAdd{});
+        if (tid == 0) sp.mass[(size_t)row * sp.parts + part] = sum;
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(FINISH_THREADS) void k_choose_split_finish(ChooseArgs a, SplitRows sp, int shift) {
+    __shared__ ChooseShared<FINISH_THREADS> sh;
+    __shared__ u64 list[LIST], part_mass[SPLIT_PARTS];
+    const int row = blockIdx.x, tid = threadIdx.x;
+    const SplitRow<T> r(a, sp, row, shift);
+    if (r.done) {
+        if (tid == 0) write_choice(a, row, r.weight.kmax ? (int)~(uint32_t)r.best : -1, r.weight.kmax ? 0.f : -INFINITY);
+        return;
+    }
+    const bool by_count = r.by_count(a.V), by_mass = r.by_mass();
+    const uint32_t listed = by_count || by_mass ? sp.listed[row] : 0;
+    if (listed > LIST || (by_count && r.st.top_k > LIST)) {
+        choose_block<T, FINISH_THREADS, 0>(a, row, shift, sh);
+        return;
+    }
+    for (uint32_t i = tid; i < listed; i += FINISH_THREADS) list[i] = sp.list[(size_t)row * LIST + i];
+    if (tid < SPLIT_PARTS) part_mass[tid] = !by_count && tid < sp.parts ? sp.mass[(size_t)row * sp.parts + tid] : 0;
+    __syncthreads();
+    const u64 least = r.weight.least(r.st.min_p);
+    u64 cut = 1ull << 32;
+    auto weight = [&](u64 o) { return r.weight((uint32_t)(o >> 32)); };
+    auto kept = [&](u64 o) {
+        const u64 w = o < cut ? 0 : weight(o);
+        return w < least ? (u64)0 : w;
+    };
+    // the list's entries from the cut on, with their values, in the order of `name`
+    auto entries = [&](auto name, auto value) {
+        return [&, name, value](auto f) {
+            for (uint32_t i = tid; i < listed; i += FINISH_THREADS)
+                if (list[i] >= cut) f(name(list[i]), value(list[i]));
+        };
+    };
+    auto order = [](u64 o) { return o; };
+    auto sum_of = [&](auto value) {
+        u64 s = 0;
+        entries(order, value)([&](u64, u64 v) { s += v; });
+        return block_reduce<FINISH_THREADS>(s, sh.tmp, OpAdd{});
+    };
+    if (by_count) {
+        if (listed > (uint32_t)r.st.top_k)
+            cut = find_entry<FINISH_THREADS>(entries(order, [](u64) -> u64 { return 1; }), (u64)r.st.top_k, sh);
+        if (by_mass) cut = find_entry<FINISH_THREADS>(entries(order, weight), mass_of(r.st.top_p, sum_of(weight)), sh);
+        const u64 total = sum_of(kept), target = target_of(r.st.u, total);
+        // (the lower half of an order key is the complement of the index: the largest is the lowest index)
+        const u64 at = find_entry<FINISH_THREADS>(entries([](u64 o) { return o & 0xffffffffull; }, kept), target + 1, sh);
+        for (uint32_t i = tid; i < listed; i += FINISH_THREADS)
+            if ((list[i] & 0xffffffffull) == at)
+                write_choice(a, row, (int)~(uint32_t)at, r.weight.log_share((uint32_t)(list[i] >> 32), total));
+        return;
+    }
+    int bin = 0;
+    if (by_mass) {
+        // what is missing of the mass in the list's bin: the bins before it hold the rest
+        u64 total = 0, before = 0;
+        const int b = tid < SPLIT_BINS ? tid : 0;
+        const u64 v = tid < SPLIT_BINS ? sp.bin_mass[(size_t)row * SPLIT_BINS + b] : 0;
+        bin = r.bin((uint32_t)(list[0] >> 32));
+        before = block_reduce<FINISH_THREADS>(tid < bin ? v : 0, sh.tmp, OpAdd{});
+        total = block_reduce<FINISH_THREADS>(v, sh.tmp, OpAdd{});
+        cut = find_entry<FINISH_THREADS>(entries(order, weight), mass_of(r.st.top_p, total) - before, sh);
+        for (uint32_t i = tid; i < listed; i += FINISH_THREADS) {
+            const u64 w = kept(list[i]);
+            if (w) atomicAdd(&part_mass[~(uint32_t)list[i] / (uint32_t)sp.per], w);
+        }
+        __syncthreads();
+    }
+    // the part in which the running sum exceeds the target
+    const int lane = tid & 63;
+    const u64 mine = part_mass[lane], run = wave_scan(mine, OpAdd{}), total = lane_value(run, 63), target = target_of(r.st.u, total);
+    const int part = __ffsll(__ballot(run > target)) - 1;
+    const u64 start = lane_value(run - mine, part);
+    RowKeys<T, FINISH_THREADS, 0> keys;
+    const int origin = part * sp.per;
+    keys.init(static_cast<const T*>(a.logits) + row * a.stride + origin, min(sp.per, a.V - origin));
+    auto kept_at = [&](int i, uint32_t k) { return k ? kept(order_key(k, origin + i)) : (u64)0; };
+    u64 sum = 0, part_total;
+    keys.each([&](int i, uint32_t k) { sum += kept_at(i, k); });
+    const u64 wave_sum = wave_reduce(sum, OpAdd{});
+    const u64 end = lane_value(block_scan<FINISH_THREADS>(lane == 63 ? wave_sum : 0, sh.tmp, part_total), 63);
+    choose_among(a, row, keys, origin, start, target, total, wave_sum, end, r.weight, kept_at);
+}
+
+// Parts of a row, 0 for rows that are not split: those of more than 8192 entries (up to there a workgroup keeps the keys in
+// its registers), as long as there are few enough rows to leave workgroups for it.
+constexpr int SPLIT_WORKGROUPS = 1024;
+int split_parts(int B, int V) {
+    if (V <= 8192 || B > SPLIT_WORKGROUPS / 4) return 0;
+    const int parts = min((V + 4095) / 4096, SPLIT_WORKGROUPS / B);
+    return min(max(parts, 1), SPLIT_PARTS);
+}
+
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+// lays the workspace out; p == nullptr: its size alone
+size_t split_layout(int B, int V, char* p, SplitRows& sp) {
+    sp.parts = split_parts(B, V);
+    if (sp.parts == 0) return 0;
+    sp.per = ((V + sp.parts - 1) / sp.parts + 3) & ~3;
+    size_t n = 0;
+    auto take = [&](auto*& field, size_t count) {
+        field = reinterpret_cast<std::remove_reference_t<decltype(field)>>(p + n);
+        n += align256(count * sizeof(*field));
+    };
+    take(sp.best, (size_t)B * sp.parts);
+    take(sp.mass, (size_t)B * sp.parts);
+    take(sp.bin_mass, (size_t)B * SPLIT_BINS);
+    take(sp.bin_count, (size_t)B * SPLIT_BINS);
+    take(sp.listed, (size_t)B);
+    take(sp.list, (size_t)B * LIST);
+    return n;
+}
+
 template <class T>
 void launch_choose_rows(const ChooseArgs& a, int shift, hipStream_t s) {
     const int V = a.V;
     const dim3 waves((a.B + 3) / 4), rows(a.B);
+    SplitRows sp;
     if (V <= 64) hipLaunchKernelGGL((k_choose_wave<T, 1, 1>), waves, dim3(256), 0, s, a, shift);
     else if (V <= 128) hipLaunchKernelGGL((k_choose_wave<T, 2, 1>), waves, dim3(256), 0, s, a, shift);
     else if (V <= 256) hipLaunchKernelGGL((k_choose_wave<T, 4, 1>), waves, dim3(256), 0, s, a, shift);
@@ -592,12 +909,24 @@ void launch_choose_rows(const ChooseArgs& a, int shift, hipStream_t s) {
     else if (V <= 1024) hipLaunchKernelGGL((k_choose_wave<T, 4, 4>), waves, dim3(256), 0, s, a, shift);
     else if (V <= 2048) hipLaunchKernelGGL((k_choose_block<T, 256, 2>), rows, dim3(256), 0, s, a, shift);
     else if (V <= 8192) hipLaunchKernelGGL((k_choose_block<T, 1024, 2>), rows, dim3(1024), 0, s, a, shift);
-    else hipLaunchKernelGGL((k_choose_block<T, 1024, 0>), rows, dim3(1024), 0, s, a, shift);
+    else if (split_layout(a.B, V, static_cast<char*>(a.workspace), sp) == 0)
+        hipLaunchKernelGGL((k_choose_block<T, 1024, 0>), rows, dim3(1024), 0, s, a, shift);
+    else {
+        const dim3 parts(a.B * sp.parts);
+        hipLaunchKernelGGL(k_choose_split_max<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp);
+        hipLaunchKernelGGL(k_choose_split_bins<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp, shift);
+        const bool filters = a.top_k.p || a.top_p.p || (a.top_k.v > 0 && a.top_k.v < V) || a.top_p.v < 1.f;
+        if (filters) hipLaunchKernelGGL(k_choose_split_collect<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp, shift);
+        hipLaunchKernelGGL(k_choose_split_finish<T>, rows, dim3(FINISH_THREADS), 0, s, a, sp, shift);
+    }
 }
 
 }  // namespace
 
-size_t choose_workspace(int, int) { return 0; }
+size_t choose_workspace(int B, int V) {
+    SplitRows sp;
+    return B > 0 ? split_layout(B, V, nullptr, sp) : 0;
+}
 
 void launch_choose(const ChooseArgs& a, hipStream_t s) {
     if (a.B == 0) return;
