@@ -389,7 +389,13 @@ struct RowKeys {
     }
 };
 
-constexpr float BIN_RANGE = 32.f;       // in units of T: a weight beyond is below 2e-14 of the largest
+// Bins per unit of the logits: over BIN_RANGE T (a weight beyond is below 2e-14 of the largest), or over the range of the
+// row's logits where that is less, so that a flat row fills its bins too.
+constexpr float BIN_RANGE = 32.f;
+__device__ __forceinline__ float bins_per_unit(float highest, float lowest, float inv_t, int bins) {
+    const float range = highest - lowest, by_t = inv_t * ((float)bins / BIN_RANGE);
+    return range > 0.f ? fmaxf(by_t, (float)bins / range) : by_t;
+}
 
 template <int NT>
 struct ChooseShared {
@@ -397,8 +403,9 @@ struct ChooseShared {
     u64 mass[BINS];
     uint32_t count[BINS];
     u64 digit[256];
-    u64 tmp[NT / 64];
-    u64 found[2];
+    uint32_t digit_count[256];
+    u64 tmp[NT / 64], tmp2[NT / 64];
+    u64 found[4];
 };
 
 template <int NT, class V, class Op>
@@ -444,23 +451,32 @@ __device__ __forceinline__ void find_bin(const C* bins, u64 target, ChooseShared
 }
 
 // Of the entries that each(f) passes to f(order key, value): the one, in descending order, at which the running sum of the
-// values reaches target.  A byte of the order key after the other, from the first in which the entries differ.
+// values reaches target.  A byte of the order key after the other, from the first in which the entries differ, until one
+// entry is left.
 template <int NT, class Each>
 __device__ __forceinline__ u64 find_entry(Each&& each, u64 target, ChooseShared<NT>& sh) {
     u64 hi = 0, lo = 0;
     each([&](u64 o, u64) { hi = max(hi, o), lo = max(lo, ~o); });
-    hi = block_reduce<NT>(hi, sh.tmp, OpMax{});
-    lo = ~block_reduce<NT>(lo, sh.tmp, OpMax{});
-    int top = 64 - __clzll(hi ^ lo);                             // bits in which they differ (0: one entry)
+    hi = wave_reduce(hi, OpMax{});
+    lo = wave_reduce(lo, OpMax{});
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh.tmp[threadIdx.x >> 6] = hi, sh.tmp2[threadIdx.x >> 6] = lo;
+    __syncthreads();
+    for (int w = 0; w < NT / 64; ++w) hi = max(hi, sh.tmp[w]), lo = max(lo, sh.tmp2[w]);
+    lo = ~lo;
     if (hi == lo) return hi;
+    int top = 64 - __clzll(hi ^ lo);                             // bits in which they differ
     u64 prefix = top < 64 ? hi >> top : 0;
     while (top > 0) {
         const int shift = max(0, top - 8), n = 1 << (top - shift);
         __syncthreads();
-        if (threadIdx.x < 256) sh.digit[threadIdx.x] = 0;
+        if (threadIdx.x < 256) sh.digit[threadIdx.x] = 0, sh.digit_count[threadIdx.x] = 0;
         __syncthreads();
         each([&](u64 o, u64 v) {
-            if ((top < 64 ? o >> top : 0) == prefix && v) atomicAdd(&sh.digit[(o >> shift) & (n - 1)], v);
+            if ((top < 64 ? o >> top : 0) == prefix && v) {
+                atomicAdd(&sh.digit[(o >> shift) & (n - 1)], v);
+                atomicAdd(&sh.digit_count[(o >> shift) & (n - 1)], 1u);
+            }
         });
         __syncthreads();
         if (threadIdx.x < 64) {                                  // from the largest digit down, four to a lane
@@ -470,7 +486,12 @@ __device__ __forceinline__ u64 find_entry(Each&& each, u64 target, ChooseShared<
             u64 before = wave_scan(sum, OpAdd{}) - sum;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                if (before < target && target <= before + v[c]) sh.found[0] = 255 - (4 * threadIdx.x + c), sh.found[1] = target - before;
+                if (before < target && target <= before + v[c]) {
+                    const int d = 255 - (4 * threadIdx.x + c);
+                    sh.found[0] = d;
+                    sh.found[1] = target - before;
+                    sh.found[2] = sh.digit_count[d];
+                }
                 before += v[c];
             }
         }
@@ -478,11 +499,18 @@ __device__ __forceinline__ u64 find_entry(Each&& each, u64 target, ChooseShared<
         prefix = (prefix << (top - shift)) | sh.found[0];
         target = sh.found[1];
         top = shift;
+        if (sh.found[2] == 1 && top > 0) {
+            each([&](u64 o, u64 v) {
+                if ((o >> top) == prefix && v) sh.found[3] = o;
+            });
+            __syncthreads();
+            return sh.found[3];
+        }
     }
     return prefix;
 }
 
-// The bin of a key: its distance from the largest logit, per_bin = bins / (BIN_RANGE T).
+// The bin of a key: its distance from the largest logit times bins_per_unit.
 template <class T>
 __device__ __forceinline__ int bin_of(const RowWeights<T>& weight, uint32_t k, float per_bin, int bins) {
     const float q = (weight.m - key_logit<T>(k)) * per_bin;
@@ -541,15 +569,17 @@ __device__ __forceinline__ void choose_block(const ChooseArgs& a, int row, int s
     RowKeys<T, NT, GROUPS> keys;
     keys.init(static_cast<const T*>(a.logits) + row * a.stride, V);
     u64 best = 0;
-    keys.each([&](int i, uint32_t k) { best = max(best, k ? order_key(k, i) : 0); });
+    uint32_t low = 0;                                            // complement of the lowest key
+    keys.each([&](int i, uint32_t k) { best = max(best, k ? order_key(k, i) : 0), low = max(low, k ? ~k : 0u); });
     best = block_reduce<NT>(best, sh.tmp, OpMax{});
+    low = block_reduce<NT>(low, sh.tmp, OpMax{});
     const uint32_t kmax = (uint32_t)(best >> 32);
     if (kmax == 0u || st.greedy) {
         if (tid == 0) write_choice(a, row, kmax ? (int)~(uint32_t)best : -1, kmax ? 0.f : -INFINITY);
         return;
     }
     const RowWeights<T> weight{kmax, key_logit<T>(kmax), st.log2e_t, shift};
-    const float per_bin = st.inv_t * ((float)BINS / BIN_RANGE);
+    const float per_bin = bins_per_unit(weight.m, key_logit<T>(~low), st.inv_t, BINS);
     auto bin = [&](uint32_t k) { return bin_of(weight, k, per_bin, BINS); };
     u64 cut = 1ull << 32;                                        // everything that is not left out
     const bool by_count = st.top_k > 0 && st.top_k < V, by_mass = st.top_p < 1.0;
@@ -628,14 +658,15 @@ __global__ __launch_bounds__(NT) void k_choose_block(ChooseArgs a, int shift) {
 //            at most LIST of them.  With top_p alone: that bin's entries do, and every part's kept mass in the bins before it
 //            is written down.
 //   finish   one workgroup per row finds the cut among the list's entries, the choice among them (top_k) or in the part in
-//            which the running sum exceeds the target.  A row whose list did not hold its entries (more than LIST entries
-//            nearly as large as each other) and one with top_k above LIST are done as a workgroup for every row does it.
-constexpr int SPLIT_THREADS = 256, SPLIT_BINS = 2 * SPLIT_THREADS, LIST = 4096, FINISH_THREADS = 1024;
+//            which the running sum exceeds the target.  A row whose list did not hold its entries (more than LIST entries, or
+//            PART_LIST of one part, nearly as large as each other) and one with top_k above LIST are done as a workgroup for every row does it.
+constexpr int SPLIT_THREADS = 256, SPLIT_BINS = 2 * SPLIT_THREADS, LIST = 4096, PART_LIST = 1024, FINISH_THREADS = 256;
 constexpr int SPLIT_PARTS = 64;                                  // at most (a lane each)
 
 struct SplitRows {
     int parts, per;
     u64* best;                   // [B][parts]
+    uint32_t* low;               // [B][parts] complements of the lowest keys
     u64* mass;                   // [B][parts]
     u64* bin_mass;               // [B][SPLIT_BINS]
     uint32_t* bin_count;         // [B][SPLIT_BINS]
@@ -657,10 +688,11 @@ struct SplitRow {
         st = row_settings(a, row);
         const int lane = threadIdx.x & 63;
         best = wave_reduce(lane < sp.parts ? sp.best[(size_t)row * sp.parts + lane] : 0, OpMax{});
+        const uint32_t low = wave_reduce(lane < sp.parts ? sp.low[(size_t)row * sp.parts + lane] : 0u, OpMax{});
         const uint32_t kmax = (uint32_t)(best >> 32);
         done = kmax == 0u || st.greedy;
         weight = RowWeights<T>{kmax, key_logit<T>(kmax), st.log2e_t, shift};
-        per_bin = st.inv_t * ((float)SPLIT_BINS / BIN_RANGE);
+        per_bin = bins_per_unit(weight.m, key_logit<T>(~low), st.inv_t, SPLIT_BINS);
     }
     __device__ __forceinline__ bool by_count(int V) const { return st.top_k > 0 && st.top_k < V; }
     __device__ __forceinline__ bool by_mass() const { return st.top_p < 1.0; }
@@ -687,9 +719,11 @@ __global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_max(ChooseArgs a
     RowKeys<T, SPLIT_THREADS, 0> keys;
     const int origin = split_part(a, sp, row, part, keys);
     u64 best = 0;
-    keys.each([&](int i, uint32_t k) { best = max(best, k ? order_key(k, origin + i) : 0); });
+    uint32_t low = 0;
+    keys.each([&](int i, uint32_t k) { best = max(best, k ? order_key(k, origin + i) : 0), low = max(low, k ? ~k : 0u); });
     best = block_reduce<SPLIT_THREADS>(best, tmp, OpMax{});
-    if (tid == 0) sp.best[(size_t)row * sp.parts + part] = best;
+    low = block_reduce<SPLIT_THREADS>(low, tmp, OpMax{});
+    if (tid == 0) sp.best[(size_t)row * sp.parts + part] = best, sp.low[(size_t)row * sp.parts + part] = low;
 }
 
 template <class T>
@@ -755,7 +789,10 @@ __device__ __forceinline__ SplitMode split_cut_bin(const ChooseArgs& a, const Sp
 template <class T>
 __global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_collect(ChooseArgs a, SplitRows sp, int shift) {
     __shared__ ChooseShared<SPLIT_THREADS> sh;
-    const int row = blockIdx.x / sp.parts, part = blockIdx.x - row * sp.parts, tid = threadIdx.x, lane = tid & 63;
+    __shared__ u64 mine[PART_LIST];                              // the part's entries of the list, in any order
+    __shared__ uint32_t n_mine, base;
+    const int row = blockIdx.x / sp.parts, part = blockIdx.x - row * sp.parts, tid = threadIdx.x;
+    if (tid == 0) n_mine = 0;                                    // (read behind the barriers of split_cut_bin)
     const SplitRow<T> r(a, sp, row, shift);
     int bin;
     u64 missing;
@@ -772,13 +809,20 @@ __global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_collect(ChooseAr
             const u64 w = r.weight(k);
             sum += w < least ? 0 : w;
         }
-        const u64 takers = __ballot(take);
-        if (!takers) return;
-        uint32_t at = 0;
-        if (lane == __ffsll(takers) - 1) at = atomicAdd(&sp.listed[row], (uint32_t)__popcll(takers));
-        at = (uint32_t)__builtin_amdgcn_readlane((int)at, __ffsll(takers) - 1) + __popcll(takers & ((1ull << lane) - 1));
-        if (take && at < LIST) sp.list[(size_t)row * LIST + at] = order_key(k, origin + i);
+        if (take) {
+            const uint32_t at = atomicAdd(&n_mine, 1u);
+            if (at < PART_LIST) mine[at] = order_key(k, origin + i);
+        }
     });
+    __syncthreads();
+    const uint32_t n = n_mine;
+    if (n > 0) {
+        // (more than this part can list are more than the list holds)
+        if (tid == 0) base = atomicAdd(&sp.listed[row], n <= PART_LIST ? n : LIST + 1);
+        __syncthreads();
+        for (uint32_t i = tid; i < min(n, (uint32_t)PART_LIST); i += SPLIT_THREADS)
+            if (base + i < LIST) sp.list[(size_t)row * LIST + base + i] = mine[i];
+    }
     if (mode == SPLIT_MASS) {
         sum = block_reduce<SPLIT_THREADS>(sum, sh.tmp, OpAdd{});
         if (tid == 0) sp.mass[(size_t)row * sp.parts + part] = sum;
@@ -836,15 +880,17 @@ __global__ __launch_bounds__(FINISH_THREADS) void k_choose_split_finish(ChooseAr
                 write_choice(a, row, (int)~(uint32_t)at, r.weight.log_share((uint32_t)(list[i] >> 32), total));
         return;
     }
-    int bin = 0;
     if (by_mass) {
         // what is missing of the mass in the list's bin: the bins before it hold the rest
         u64 total = 0, before = 0;
-        const int b = tid < SPLIT_BINS ? tid : 0;
-        const u64 v = tid < SPLIT_BINS ? sp.bin_mass[(size_t)row * SPLIT_BINS + b] : 0;
-        bin = r.bin((uint32_t)(list[0] >> 32));
-        before = block_reduce<FINISH_THREADS>(tid < bin ? v : 0, sh.tmp, OpAdd{});
-        total = block_reduce<FINISH_THREADS>(v, sh.tmp, OpAdd{});
+        const int bin = r.bin((uint32_t)(list[0] >> 32));
+        for (int b = tid; b < SPLIT_BINS; b += FINISH_THREADS) {
+            const u64 v = sp.bin_mass[(size_t)row * SPLIT_BINS + b];
+            total += v;
+            before += b < bin ? v : 0;
+        }
+        before = block_reduce<FINISH_THREADS>(before, sh.tmp, OpAdd{});
+        total = block_reduce<FINISH_THREADS>(total, sh.tmp, OpAdd{});
         cut = find_entry<FINISH_THREADS>(entries(order, weight), mass_of(r.st.top_p, total) - before, sh);
         for (uint32_t i = tid; i < listed; i += FINISH_THREADS) {
             const u64 w = kept(list[i]);
@@ -889,6 +935,7 @@ size_t split_layout(int B, int V, char* p, SplitRows& sp) {
         n += align256(count * sizeof(*field));
     };
     take(sp.best, (size_t)B * sp.parts);
+    take(sp.low, (size_t)B * sp.parts);
     take(sp.mass, (size_t)B * sp.parts);
     take(sp.bin_mass, (size_t)B * SPLIT_BINS);
     take(sp.bin_count, (size_t)B * SPLIT_BINS);
