@@ -260,16 +260,28 @@ __global__ __launch_bounds__(256) void k_choose_wave(ChooseArgs a, int shift) {
         }
     }
     if (st.top_p < 1.0) {
+        // Sums of the weights' upper halves (2^31 units) decide where they can: what the lower halves add is below V of them.
+        uint32_t upper[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) upper[e] = (uint32_t)(w[e] >> 31);
         const u64 mass = mass_of(st.top_p, mass_from(1));
         uint32_t lo = 1, hi = kmax + 1;                          // at least `mass` from lo on, less from hi on
         int n_lo = count_from(1), n_hi = 0;
-        u64 m_hi = 0;
-        while (hi - lo > 1 && n_lo - n_hi > 1) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            const u64 m = mass_from(mid);
+        float guess = 2.f;                                       // the cut's distance from the largest in units of T, as a start
+        for (int step = 0; hi - lo > 1 && n_lo - n_hi > 1; ++step) {
+            uint32_t mid = lo + (hi - lo) / 2;
+            if (step < 2) {
+                const uint32_t near = __builtin_amdgcn_readfirstlane((int)logit_key<float>(weight.m - guess / st.inv_t)) >> KEY_SHIFT<T>;
+                if (near > lo && near < hi) mid = near;
+            }
+            uint32_t part = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) part += k[e] >= mid ? upper[e] : 0u;
+            const u64 sum = wave_reduce(part, OpAdd{});
+            const bool enough = (sum << 31) >= mass || (((sum + V) << 31) > mass && mass_from(mid) >= mass);
             const int n = count_from(mid);
-            if (m >= mass) lo = mid, n_lo = n;
-            else hi = mid, n_hi = n, m_hi = m;
+            if (enough) lo = mid, n_lo = n, guess = 0.5f;
+            else hi = mid, n_hi = n, guess = 8.f;
         }
         if (n_lo - n_hi <= 1) {
 #pragma unroll
@@ -277,7 +289,7 @@ __global__ __launch_bounds__(256) void k_choose_wave(ChooseArgs a, int shift) {
                 if (k[e] < lo) k[e] = 0u, w[e] = 0;
         } else {
             // several of one key: as many as it takes to reach the mass
-            const u64 each = weight(lo), missing = mass - m_hi;
+            const u64 each = weight(lo), missing = mass - mass_from(hi);
             cut_at(lo, (int)((missing + each - 1) / each));
         }
     }
