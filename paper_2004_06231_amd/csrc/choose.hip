@@ -4,9 +4,9 @@
 // kept is one prefix: the entries whose order key is at least `cut`.  The order key of entry i has the logit's bits, made
 // monotone, in its upper half and ~i in its lower half: no two are equal, and the larger comes first.
 //
-// Weights exp((logit - max) / T) are held as integers of 2^-shift, shift = 62 - ceil(log2 V): at most 2^62 in all, so
+// Weights exp((logit - max) / T) are held as integers of 2^-shift, shift = 61 - ceil(log2 V): at most 2^61 in all, so
 // that their sums are exact and the same in whatever order they are formed, by atomics too.  A weight is off by half a unit
-// at most, 2^-63 of V times the largest; sums of float64 lose more where V is below 2^10, and no sum of float32 could tell
+// at most, 2^-61 of V times the largest; sums of float64 lose more where V is below 2^10, and no sum of float32 could tell
 // the entries of a long row apart: a uniform falls between two of V running sums.
 #include "device_common.hpp"
 #include "routing.hpp"
@@ -62,29 +62,49 @@ __device__ __forceinline__ RowSettings row_settings(const ChooseArgs& a, int row
     return s;
 }
 
-// 2^y in units of 2^-shift, rounded to the nearest, for y <= 0.  2^y = 2^n 2^f with n the nearest integer: the series of 2^f =
-// exp(f ln 2) to the 12th power is good to 0.347^13 / 13! = 1.7e-16.  Added to 2 its last place is 2^-51, whole.
-__device__ __forceinline__ u64 exp2_fixed(double y, int shift) {
+// 2^y in units of 2^-shift, shift <= 61, rounded to the nearest, for y <= 0 (0 for NaN).  2^y = 2^n 2^f with n the nearest integer: the
+// series of 2^f = exp(f ln 2) to the 12th power is good to 0.347^13 / 13! = 1.7e-16.  Added to 2 its last place is 2^-51,
+// whole.  (The coefficients are kept in scalar registers: as literals each takes two moves before its multiplication.)
+__device__ __forceinline__ double scalar_constant(double c) {
+    asm("" : "+s"(c));
+    return c;
+}
+struct Exp2Series {
+    double c[12];
+    __device__ __forceinline__ Exp2Series() {
+        constexpr double L = 0.69314718055994530942;
+        double term = 1.0;
+#pragma unroll
+        for (int i = 1; i <= 12; ++i) {
+            term = term * L / i;
+            c[i - 1] = scalar_constant(term);
+        }
+    }
+};
+__device__ __forceinline__ u64 exp2_fixed(double y, int shift, const Exp2Series& series) {
     y = fmax(y, -128.0);
     const double n = rint(y), f = y - n;
-    constexpr double L = 0.69314718055994530942;
-    double p = L * L * L * L * L * L * L * L * L * L * L * L / 479001600.0;
-    p = fma(p, f, L * L * L * L * L * L * L * L * L * L * L / 39916800.0);
-    p = fma(p, f, L * L * L * L * L * L * L * L * L * L / 3628800.0);
-    p = fma(p, f, L * L * L * L * L * L * L * L * L / 362880.0);
-    p = fma(p, f, L * L * L * L * L * L * L * L / 40320.0);
-    p = fma(p, f, L * L * L * L * L * L * L / 5040.0);
-    p = fma(p, f, L * L * L * L * L * L / 720.0);
-    p = fma(p, f, L * L * L * L * L / 120.0);
-    p = fma(p, f, L * L * L * L / 24.0);
-    p = fma(p, f, L * L * L / 6.0);
-    p = fma(p, f, L * L / 2.0);
-    p = fma(p, f, L);
+    double p = series.c[11];
+#pragma unroll
+    for (int i = 10; i >= 0; --i) p = fma(p, f, series.c[i]);
     p = fma(p, f, 1.0);
-    const u64 i = __builtin_bit_cast(u64, p + 2.0) & 0xfffffffffffffull;       // p * 2^51
-    const int up = (int)n + shift - 51;
-    const int down = min(-up, 63);
-    return up >= 0 ? i << up : (i + (1ull << (down - 1))) >> down;
+    const u64 whole = (__builtin_bit_cast(u64, p + 2.0) & 0xfffffffffffffull) << 10;      // p * 2^61
+    const int down = min(61 - shift - (int)n, 63);               // (63: at most a quarter of a unit, which gives 0)
+    return (whole + ((1ull << down) >> 1)) >> down;
+}
+
+// log x for a positive, normal x: x = 2^e m with m between sqrt(1/2) and sqrt(2), log m = 2 atanh r with r = (m - 1) / (m + 1),
+// |r| <= 0.172: of the series in r^2 the terms up to r^19 are good to 2 * 0.172^21 / 21 = 8e-18.
+__device__ __forceinline__ double log_of(double x) {
+    const u64 b = __builtin_bit_cast(u64, x);
+    int e = (int)(b >> 52) - 1023;
+    double m = __builtin_bit_cast(double, (b & 0xfffffffffffffull) | 0x3ff0000000000000ull);
+    if (m > 1.41421356237309505) m *= 0.5, e += 1;
+    const double r = (m - 1.0) / (m + 1.0), q = r * r;
+    double s = 1.0 / 19.0;
+#pragma unroll
+    for (int i = 17; i >= 1; i -= 2) s = fma(s, q, 1.0 / i);
+    return fma((double)e, 0.69314718055994530942, 2.0 * r * s);
 }
 
 // What the weights of a row are computed from.
@@ -94,14 +114,16 @@ struct RowWeights {
     float m;                     // the largest logit
     double log2e_t;
     int shift;
-    // (only entries at +inf have weight next to one)
-    __device__ __forceinline__ u64 operator()(uint32_t k) const {
-        if (k == 0u || (m == INFINITY && k != kmax)) return 0;
-        return exp2_fixed(k == kmax ? 0.0 : ((double)key_logit<T>(k) - (double)m) * log2e_t, shift);
+    // (Key 0 stands for a NaN, which has no weight.  Next to an entry at +inf the others are infinitely far.)
+    __device__ __forceinline__ double exponent(uint32_t k) const {
+        const double y = ((double)key_logit<T>(k) - (double)m) * log2e_t;
+        return k == kmax ? 0.0 : y;
+    }
+    __device__ __forceinline__ u64 operator()(uint32_t k, const Exp2Series& series = Exp2Series()) const {
+        return exp2_fixed(exponent(k), shift, series);
     }
     __device__ __forceinline__ float log_share(uint32_t k, u64 total) const {
-        const double d = k == kmax ? 0.0 : ((double)key_logit<T>(k) - (double)m) * log2e_t * 0.69314718055994530942;
-        return (float)(d - log((double)total * exp2((double)-shift)));
+        return (float)(exponent(k) * 0.69314718055994530942 - log_of(ldexp((double)total, -shift)));
     }
     // the least weight that min_p keeps
     __device__ __forceinline__ u64 least(double min_p) const { return __double2ull_ru(min_p * (double)(1ull << shift)); }
@@ -204,8 +226,11 @@ __global__ __launch_bounds__(256) void k_choose_wave(ChooseArgs a, int shift) {
     }
     const RowWeights<T> weight{kmax, key_logit<T>(kmax), st.log2e_t, shift};
     u64 w[E];
+    {
+        const Exp2Series series;
 #pragma unroll
-    for (int e = 0; e < E; ++e) w[e] = weight(k[e]);
+        for (int e = 0; e < E; ++e) w[e] = weight(k[e], series);
+    }
     // entries of key t beyond the first `keep` of them go, and all below t
     auto cut_at = [&](uint32_t t, int keep) {
         int before = 0;
@@ -991,7 +1016,7 @@ void launch_choose(const ChooseArgs& a, hipStream_t s) {
     if (a.B == 0) return;
     int log_v = 0;
     while (((int64_t)1 << log_v) < a.V) ++log_v;
-    const int shift = 62 - log_v;
+    const int shift = 61 - log_v;
     if (a.type == ROW_FLOAT32) launch_choose_rows<float>(a, shift, s);
     else if (a.type == ROW_BFLOAT16) launch_choose_rows<__bf16>(a, shift, s);
     else launch_choose_rows<_Float16>(a, shift, s);

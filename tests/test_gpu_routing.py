@@ -13,8 +13,8 @@ Tolerances.  u = 2^-24 is half a step of float32.
   dweights  products and sums over a row of H: at most H / 64 + 64 additions in a lane and 16 across: u (H / 64 + 82) of
             the sum of magnitudes.
   choose    the index is the oracle's; its log-share comes from float64 numbers (2^-36 for their sums and logarithms, which stay
-            below 2^7) and from a total of V weights, each rounded to a multiple of 2^-(62 - ceil(log2 V)) of the largest: off
-            by V / 2 such units of a total of one at least, rounded once: u |logq| + 2^-36 + V 2^-(63 - ceil(log2 V)).
+            below 2^7) and from a total of V weights, each rounded to a multiple of 2^-(61 - ceil(log2 V)) of the largest: off
+            by V / 2 such units of a total of one at least, rounded once: u |logq| + 2^-36 + V 2^-(62 - ceil(log2 V)).
 """
 import math
 
@@ -262,7 +262,7 @@ def check_choose(logits, u, **settings):
     assert host(index).tolist() == [i for i, _ in want]
     q = np.array([v for _, v in want])
     V = x.shape[1]
-    close(logq, q, U * np.where(np.isfinite(q), np.abs(q), 0) + 2.0 ** -36 + V * 2.0 ** -(63 - (V - 1).bit_length()))
+    close(logq, q, U * np.where(np.isfinite(q), np.abs(q), 0) + 2.0 ** -36 + V * 2.0 ** -(62 - (V - 1).bit_length()))
     return index
 
 
