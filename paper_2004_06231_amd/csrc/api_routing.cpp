@@ -194,7 +194,7 @@ int einet_choose(const void* logit_dev, int dtype, int64_t row_stride, int n_row
     if (need > 0 && (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < need))
         return invalid(call, "needs a workspace of einet_choose_workspace bytes, 256-byte aligned");
     launch_choose(ChooseArgs{logit_dev, dtype, row_stride, n_rows, n_entries, u_dev, {temperature_dev, temperature},
-                             {top_p_dev, top_p}, {min_p_dev, min_p}, {top_k_dev, top_k}, index_dev, logq_dev, workspace_dev},
+                             {top_p_dev, top_p}, {min_p_dev, min_p}, {top_k_dev, top_k}, index_dev, logq_dev, workspace_dev, 0.f, 0.0},
                   static_cast<hipStream_t>(stream));
     return check_hip(call);
 }

@@ -26,8 +26,7 @@ template <> constexpr int KEY_SHIFT<__bf16> = 16;
 template <> constexpr int KEY_SHIFT<_Float16> = 13;
 
 template <class T>
-__device__ __forceinline__ uint32_t logit_key(T x) {
-    const float v = (float)x;
+__device__ __forceinline__ uint32_t logit_key(float v) {
     uint32_t b = __builtin_bit_cast(uint32_t, v);
     if (v == 0.f) b = 0u;                                        // -0 and 0 are equal
     const uint32_t k = ((b >> 31) ? ~b : b | 0x80000000u) >> KEY_SHIFT<T>;
@@ -42,19 +41,25 @@ __device__ __forceinline__ float key_logit(uint32_t k) {
 __device__ __forceinline__ u64 order_key(uint32_t k, int i) { return ((u64)k << 32) | (uint32_t)~i; }
 
 struct RowSettings {
-    float inv_t;                 // 1 / T in float32, for the bins
+    float t, inv_t;              // T and 1 / T in float32, for the bins
     double log2e_t;              // log2(e) / T
     int top_k;
     double top_p, min_p, u;
     bool greedy;
 };
 __device__ __forceinline__ RowSettings row_settings(const ChooseArgs& a, int row) {
-    const float t = a.temperature.p ? a.temperature.p[row] : a.temperature.v, p = a.top_p.p ? a.top_p.p[row] : a.top_p.v,
-                mp = a.min_p.p ? a.min_p.p[row] : a.min_p.v, u = a.u[row];
+    const float p = a.top_p.p ? a.top_p.p[row] : a.top_p.v, mp = a.min_p.p ? a.min_p.p[row] : a.min_p.v, u = a.u[row];
     RowSettings s;
-    s.greedy = !(t > 0.f);
-    s.inv_t = s.greedy ? 1.f : 1.f / t;
-    s.log2e_t = 1.4426950408889634074 / (s.greedy ? 1.0 : (double)t);
+    if (a.temperature.p) {
+        s.t = a.temperature.p[row];
+        s.inv_t = 1.f / s.t;
+        s.log2e_t = 1.4426950408889634074 / (double)s.t;
+    } else {
+        s.t = a.temperature.v;
+        s.inv_t = a.inv_t;                                       // (divided once, by the host)
+        s.log2e_t = a.log2e_t;
+    }
+    s.greedy = !(s.t > 0.f);
     s.top_k = a.top_k.p ? a.top_k.p[row] : a.top_k.v;
     s.top_p = p >= 0.f ? (double)p : p < 0.f ? 0.0 : 1.0;       // (NaN: off)
     s.min_p = mp > 0.f ? fmin((double)mp, 1.0) : 0.0;
@@ -114,16 +119,14 @@ struct RowWeights {
     float m;                     // the largest logit
     double log2e_t;
     int shift;
-    // (Key 0 stands for a NaN, which has no weight.  Next to an entry at +inf the others are infinitely far.)
-    __device__ __forceinline__ double exponent(uint32_t k) const {
-        const double y = ((double)key_logit<T>(k) - (double)m) * log2e_t;
-        return k == kmax ? 0.0 : y;
+    // (a NaN has no weight; next to an entry at +inf the others are infinitely far)
+    __device__ __forceinline__ double exponent(float v) const { return v == m ? 0.0 : ((double)v - (double)m) * log2e_t; }
+    __device__ __forceinline__ u64 operator()(float v, const Exp2Series& series = Exp2Series()) const {
+        return exp2_fixed(exponent(v), shift, series);
     }
-    __device__ __forceinline__ u64 operator()(uint32_t k, const Exp2Series& series = Exp2Series()) const {
-        return exp2_fixed(exponent(k), shift, series);
-    }
-    __device__ __forceinline__ float log_share(uint32_t k, u64 total) const {
-        return (float)(exponent(k) * 0.69314718055994530942 - log_of(ldexp((double)total, -shift)));
+    __device__ __forceinline__ u64 of_key(uint32_t k) const { return (*this)(key_logit<T>(k)); }
+    __device__ __forceinline__ float log_share(float v, u64 total) const {
+        return (float)(exponent(v) * 0.69314718055994530942 - log_of(ldexp((double)total, -shift)));
     }
     // the least weight that min_p keeps
     __device__ __forceinline__ u64 least(double min_p) const { return __double2ull_ru(min_p * (double)(1ull << shift)); }
@@ -138,17 +141,17 @@ __device__ __forceinline__ u64 target_of(double u, u64 total) {
 // the mass that the entries kept by top_p reach, 1 .. total
 __device__ __forceinline__ u64 mass_of(double top_p, u64 total) { return max((u64)1, __double2ull_ru(top_p * (double)total)); }
 
-// N consecutive entries of a row, of which the first `count` exist; the hardware loads them at any alignment at once
+// N consecutive entries of a row, of which the first `count` exist (the others are -inf)
 template <class T, int N>
-__device__ __forceinline__ void load_keys(const T* x, int count, uint32_t (&k)[N]) {
+__device__ __forceinline__ void load_logits(const T* x, int count, float (&v)[N]) {
     struct Pack { T v[N]; };
     if (count >= N) {
         const Pack q = load_bytes<Pack>(x);
 #pragma unroll
-        for (int c = 0; c < N; ++c) k[c] = logit_key(q.v[c]);
+        for (int c = 0; c < N; ++c) v[c] = (float)q.v[c];
     } else {
 #pragma unroll
-        for (int c = 0; c < N; ++c) k[c] = c < count ? logit_key(x[c]) : 0u;
+        for (int c = 0; c < N; ++c) v[c] = c < count ? (float)x[c] : -INFINITY;
     }
 }
 
@@ -200,15 +203,20 @@ __global__ __launch_bounds__(256) void k_choose_wave(ChooseArgs a, int shift) {
     if (row >= a.B) return;
     const T* const x = static_cast<const T*>(a.logits) + row * a.stride;
     const RowSettings st = row_settings(a, row);
+    float v[E];
     uint32_t k[E];
     uint32_t best = 0;
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
-        uint32_t part[VEC];
+        float part[VEC];
         const int i0 = (g * 64 + lane) * VEC;
-        load_keys<T, VEC>(x + i0, V - i0, part);
+        load_logits<T, VEC>(x + i0, V - i0, part);
 #pragma unroll
-        for (int c = 0; c < VEC; ++c) k[g * VEC + c] = part[c], best = max(best, part[c]);
+        for (int c = 0; c < VEC; ++c) {
+            v[g * VEC + c] = part[c];
+            k[g * VEC + c] = logit_key<T>(part[c]);
+            best = max(best, k[g * VEC + c]);
+        }
     }
     const uint32_t kmax = wave_reduce(best, OpMax{});
     auto index_of = [&](int e) { return ((e / VEC) * 64 + lane) * VEC + e % VEC; };
@@ -229,7 +237,7 @@ __global__ __launch_bounds__(256) void k_choose_wave(ChooseArgs a, int shift) {
     {
         const Exp2Series series;
 #pragma unroll
-        for (int e = 0; e < E; ++e) w[e] = weight(k[e], series);
+        for (int e = 0; e < E; ++e) w[e] = weight(v[e], series);
     }
     // entries of key t beyond the first `keep` of them go, and all below t
     auto cut_at = [&](uint32_t t, int keep) {
@@ -296,7 +304,7 @@ __global__ __launch_bounds__(256) void k_choose_wave(ChooseArgs a, int shift) {
         for (int step = 0; hi - lo > 1 && n_lo - n_hi > 1; ++step) {
             uint32_t mid = lo + (hi - lo) / 2;
             if (step < 2) {
-                const uint32_t near = __builtin_amdgcn_readfirstlane((int)logit_key<float>(weight.m - guess / st.inv_t)) >> KEY_SHIFT<T>;
+                const uint32_t near = __builtin_amdgcn_readfirstlane((int)logit_key<T>(weight.m - guess * st.t));
                 if (near > lo && near < hi) mid = near;
             }
             uint32_t part = 0;
@@ -314,7 +322,7 @@ __global__ __launch_bounds__(256) void k_choose_wave(ChooseArgs a, int shift) {
                 if (k[e] < lo) k[e] = 0u, w[e] = 0;
         } else {
             // several of one key: as many as it takes to reach the mass
-            const u64 each = weight(lo), missing = mass - mass_from(hi);
+            const u64 each = weight.of_key(lo), missing = mass - mass_from(hi);
             cut_at(lo, (int)((missing + each - 1) / each));
         }
     }
@@ -353,7 +361,7 @@ __global__ __launch_bounds__(256) void k_choose_wave(ChooseArgs a, int shift) {
                 for (int c = 0; c < VEC; ++c)
                     if (c == at) key = k[g * VEC + c];
                 a.index[row] = (g * 64 + lane) * VEC + at;
-                if (a.logq) a.logq[row] = weight.log_share(key, total);
+                if (a.logq) a.logq[row] = weight.log_share(key_logit<T>(key), total);
             }
         }
     }
@@ -362,17 +370,16 @@ __global__ __launch_bounds__(256) void k_choose_wave(ChooseArgs a, int shift) {
 // ------------------------------------------------------------------------------------------ a workgroup for every row
 //
 // Wave w of the workgroup has a contiguous stretch of the row, in groups of 256 entries (four to a lane).  GROUPS > 0: the
-// keys of the stretch stay in registers; 0: they are read again by every pass.
+// logits of the stretch stay in registers; 0: they are read again by every pass.
 //
 // A cut is found from the histogram of the entries over their distance from the largest logit in units of T (BINS equal bins
 // to 32 units; their order is the entries' order): the bin that the cut lies in holds few entries of an ordinary row, and a
 // radix search over the order keys of that bin's entries finds the very entry.
 template <class T, int NT, int GROUPS>
-struct RowKeys {
+struct RowLogits {
     const T* x;
     int V, first, groups;        // of this thread's wave: its first group, the number of its groups
-    uint32_t k[GROUPS > 0 ? GROUPS * 4 : 1];
-    // entries 0 .. n-1 of row; another origin only moves the indexes that the caller adds
+    float v[GROUPS > 0 ? GROUPS * 4 : 1];
     __device__ __forceinline__ void init(const T* row, int n) {
         x = row;
         V = n;
@@ -382,11 +389,10 @@ struct RowKeys {
             first = wave * GROUPS;
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) {
-                uint32_t part[4];
-                const int i0 = (first + g) * 256 + (int)(threadIdx.x & 63) * 4;
-                load_keys<T, 4>(x + i0, V - i0, part);
+                float part[4];
+                load_logits<T, 4>(x + index(g), V - index(g), part);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) k[g * 4 + c] = part[c];
+                for (int c = 0; c < 4; ++c) v[g * 4 + c] = part[c];
             }
         } else {
             groups = (V + NT * 4 - 1) / (NT * 4);
@@ -394,14 +400,13 @@ struct RowKeys {
         }
     }
     __device__ __forceinline__ int index(int g) const { return (first + g) * 256 + (int)(threadIdx.x & 63) * 4; }
-    // f(index, key) for the four entries of a group
+    // f(index, logit) for the four entries of a group
     template <class F>
     __device__ __forceinline__ void group(int g, F&& f) const {
-        const int i0 = index(g);
-        uint32_t part[4];
-        load_keys<T, 4>(x + i0, V - i0, part);
+        float part[4];
+        load_logits<T, 4>(x + index(g), V - index(g), part);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) f(i0 + c, part[c]);
+        for (int c = 0; c < 4; ++c) f(index(g) + c, part[c]);
     }
     template <class F>
     __device__ __forceinline__ void each(F&& f) const {
@@ -409,13 +414,13 @@ struct RowKeys {
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) f(index(g) + c, k[g * 4 + c]);
+                for (int c = 0; c < 4; ++c) f(index(g) + c, v[g * 4 + c]);
         } else {
             int g = 0;
             for (; g + 4 <= groups; g += 4) {                    // (four loads in flight)
-                uint32_t part[4][4];
+                float part[4][4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) load_keys<T, 4>(x + index(g + q), V - index(g + q), part[q]);
+                for (int q = 0; q < 4; ++q) load_logits<T, 4>(x + index(g + q), V - index(g + q), part[q]);
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -547,11 +552,29 @@ __device__ __forceinline__ u64 find_entry(Each&& each, u64 target, ChooseShared<
     return prefix;
 }
 
-// The bin of a key: its distance from the largest logit times bins_per_unit.
+// The bin of a logit: its distance from the largest times bins_per_unit.
 template <class T>
-__device__ __forceinline__ int bin_of(const RowWeights<T>& weight, uint32_t k, float per_bin, int bins) {
-    const float q = (weight.m - key_logit<T>(k)) * per_bin;
-    return k == weight.kmax ? 0 : q < (float)(bins - 1) ? (int)q : bins - 1;
+__device__ __forceinline__ int bin_of(const RowWeights<T>& weight, float v, float per_bin, int bins) {
+    const float q = (weight.m - v) * per_bin;
+    return v == weight.m ? 0 : q < (float)(bins - 1) ? (int)q : bins - 1;
+}
+
+// The largest order key of the entries and the complement of the lowest key, over the workgroup (0 without an entry).
+template <class T, int NT, class Row>
+__device__ __forceinline__ void row_ends(const Row& row, int origin, u64* tmp, u64* tmp2, u64& best, uint32_t& low) {
+    best = 0;
+    low = 0;
+    row.each([&](int i, float v) {
+        const uint32_t k = logit_key<T>(v);
+        best = max(best, k ? order_key(k, origin + i) : 0);
+        low = max(low, k ? ~k : 0u);
+    });
+    best = wave_reduce(best, OpMax{});
+    low = wave_reduce(low, OpMax{});
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = best, tmp2[threadIdx.x >> 6] = low;
+    __syncthreads();
+    for (int w = 0; w < NT / 64; ++w) best = max(best, tmp[w]), low = max(low, (uint32_t)tmp2[w]);
 }
 
 __device__ __forceinline__ void write_choice(const ChooseArgs& a, int row, int index, float logq) {
@@ -559,10 +582,10 @@ __device__ __forceinline__ void write_choice(const ChooseArgs& a, int row, int i
     if (a.logq) a.logq[row] = logq;
 }
 
-// The choice among the entries of `keys` (those of the row from `origin` on), of which kept(index, key) is the kept weight:
+// The choice among the entries of `keys` (those of the row from `origin` on), of which kept(index, logit) is the kept weight:
 // the first at which the running sum, `before` at the start, exceeds target.  total: of all kept weights of the row.
 template <class T, int NT, int GROUPS, class Kept>
-__device__ __forceinline__ void choose_among(const ChooseArgs& a, int row, const RowKeys<T, NT, GROUPS>& keys, int origin, u64 before,
+__device__ __forceinline__ void choose_among(const ChooseArgs& a, int row, const RowLogits<T, NT, GROUPS>& keys, int origin, u64 before,
                                              u64 target, u64 total, u64 wave_sum, u64 wave_end, const RowWeights<T>& weight,
                                              Kept&& kept) {
     // the wave in whose stretch that is goes through its groups
@@ -570,11 +593,11 @@ __device__ __forceinline__ void choose_among(const ChooseArgs& a, int row, const
     if (target < run || target >= run + wave_sum) return;
     for (int g = 0; g < keys.groups; ++g) {
         u64 w[4], sum = 0;
-        uint32_t k4[4];
+        float v4[4];
         int c = 0;
-        keys.group(g, [&](int i, uint32_t k) {
-            k4[c] = k;
-            w[c] = kept(i, k);
+        keys.group(g, [&](int i, float v) {
+            v4[c] = v;
+            w[c] = kept(i, v);
             sum += w[c];
             ++c;
         });
@@ -589,8 +612,8 @@ __device__ __forceinline__ void choose_among(const ChooseArgs& a, int row, const
                     s -= w[q];                                   // the running sum at place q - 1
                     if (s > target) at = q - 1;
                 }
-                const uint32_t key = at == 0 ? k4[0] : at == 1 ? k4[1] : at == 2 ? k4[2] : k4[3];
-                write_choice(a, row, origin + keys.index(g) + at, weight.log_share(key, total));
+                const float v = at == 0 ? v4[0] : at == 1 ? v4[1] : at == 2 ? v4[2] : v4[3];
+                write_choice(a, row, origin + keys.index(g) + at, weight.log_share(v, total));
             }
             return;
         }
@@ -603,13 +626,11 @@ __device__ __forceinline__ void choose_block(const ChooseArgs& a, int row, int s
     constexpr int BINS = ChooseShared<NT>::BINS;
     const int tid = threadIdx.x, V = a.V;
     const RowSettings st = row_settings(a, row);
-    RowKeys<T, NT, GROUPS> keys;
+    RowLogits<T, NT, GROUPS> keys;
     keys.init(static_cast<const T*>(a.logits) + row * a.stride, V);
-    u64 best = 0;
-    uint32_t low = 0;                                            // complement of the lowest key
-    keys.each([&](int i, uint32_t k) { best = max(best, k ? order_key(k, i) : 0), low = max(low, k ? ~k : 0u); });
-    best = block_reduce<NT>(best, sh.tmp, OpMax{});
-    low = block_reduce<NT>(low, sh.tmp, OpMax{});
+    u64 best;
+    uint32_t low;
+    row_ends<T, NT>(keys, 0, sh.tmp, sh.tmp2, best, low);
     const uint32_t kmax = (uint32_t)(best >> 32);
     if (kmax == 0u || st.greedy) {
         if (tid == 0) write_choice(a, row, kmax ? (int)~(uint32_t)best : -1, kmax ? 0.f : -INFINITY);
@@ -617,26 +638,26 @@ __device__ __forceinline__ void choose_block(const ChooseArgs& a, int row, int s
     }
     const RowWeights<T> weight{kmax, key_logit<T>(kmax), st.log2e_t, shift};
     const float per_bin = bins_per_unit(weight.m, key_logit<T>(~low), st.inv_t, BINS);
-    auto bin = [&](uint32_t k) { return bin_of(weight, k, per_bin, BINS); };
+    auto bin = [&](float v) { return bin_of(weight, v, per_bin, BINS); };
     u64 cut = 1ull << 32;                                        // everything that is not left out
     const bool by_count = st.top_k > 0 && st.top_k < V, by_mass = st.top_p < 1.0;
     if (by_count || by_mass) {
         for (int b = tid; b < BINS; b += NT) sh.count[b] = 0, sh.mass[b] = 0;
         __syncthreads();
-        keys.each([&](int, uint32_t k) {
-            if (k == 0u) return;
-            const int b = bin(k);
+        keys.each([&](int, float v) {
+            if (!(v > -INFINITY)) return;
+            const int b = bin(v);
             if (by_count) atomicAdd(&sh.count[b], 1u);
-            if (by_mass) atomicAdd(&sh.mass[b], weight(k));
+            if (by_mass) atomicAdd(&sh.mass[b], weight(v));
         });
         __syncthreads();
         // entries of a bin from the cut on, with their values
         auto of_bin = [&](int at, auto value) {
             return [&, at, value](auto f) {
-                keys.each([&](int i, uint32_t k) {
-                    if (k == 0u || bin(k) != at) return;
-                    const u64 o = order_key(k, i);
-                    if (o >= cut) f(o, value(k));
+                keys.each([&](int i, float v) {
+                    if (!(v > -INFINITY) || bin(v) != at) return;
+                    const u64 o = order_key(logit_key<T>(v), i);
+                    if (o >= cut) f(o, value(v));
                 });
             };
         };
@@ -646,7 +667,7 @@ __device__ __forceinline__ void choose_block(const ChooseArgs& a, int row, int s
             block_scan<NT>((u64)sh.count[2 * tid] + sh.count[2 * tid + 1], sh.tmp, total);
             if (total > (u64)st.top_k) {
                 find_bin<NT>(sh.count, (u64)st.top_k, sh, at, missing);
-                cut = find_entry<NT>(of_bin(at, [](uint32_t) -> u64 { return 1; }), missing, sh);
+                cut = find_entry<NT>(of_bin(at, [](float) -> u64 { return 1; }), missing, sh);
                 if (by_mass) {
                     // the mass of that bin is what is kept of it, that of the bins behind it none
                     u64 rest = 0;
@@ -666,20 +687,20 @@ __device__ __forceinline__ void choose_block(const ChooseArgs& a, int row, int s
         }
     }
     const u64 least = weight.least(st.min_p);
-    auto kept = [&](int i, uint32_t k) {
-        if (k == 0u || order_key(k, i) < cut) return (u64)0;
-        const u64 w = weight(k);
+    auto kept = [&](int i, float v) {
+        if (!(v > -INFINITY) || order_key(logit_key<T>(v), i) < cut) return (u64)0;
+        const u64 w = weight(v);
         return w < least ? (u64)0 : w;
     };
     u64 mine = 0, total;
-    keys.each([&](int i, uint32_t k) { mine += kept(i, k); });
+    keys.each([&](int i, float v) { mine += kept(i, v); });
     const u64 wave_sum = wave_reduce(mine, OpAdd{});
     const u64 end = lane_value(block_scan<NT>((tid & 63) == 63 ? wave_sum : 0, sh.tmp, total), 63);
     choose_among(a, row, keys, 0, 0, target_of(st.u, total), total, wave_sum, end, weight, kept);
 }
 
 template <class T, int NT, int GROUPS>
-__global__ __launch_bounds__(NT) void k_choose_block(ChooseArgs a, int shift) {
+__global__ __launch_bounds__(NT, 4) void k_choose_block(ChooseArgs a, int shift) {
     __shared__ ChooseShared<NT> sh;
     choose_block<T, NT, GROUPS>(a, blockIdx.x, shift, sh);
 }
@@ -699,12 +720,13 @@ __global__ __launch_bounds__(NT) void k_choose_block(ChooseArgs a, int shift) {
 //            PART_LIST of one part, nearly as large as each other) and one with top_k above LIST are done as a workgroup for every row does it.
 constexpr int SPLIT_THREADS = 256, SPLIT_BINS = 2 * SPLIT_THREADS, LIST = 4096, PART_LIST = 1024, FINISH_THREADS = 256;
 constexpr int SPLIT_PARTS = 64;                                  // at most (a lane each)
+constexpr int STRETCHES = SPLIT_THREADS / 64;                    // of a part: its waves'
 
 struct SplitRows {
-    int parts, per;
+    int parts, per;              // per: a multiple of 4 * SPLIT_THREADS
     u64* best;                   // [B][parts]
     uint32_t* low;               // [B][parts] complements of the lowest keys
-    u64* mass;                   // [B][parts]
+    u64* mass;                   // [B][parts][STRETCHES] kept masses
     u64* bin_mass;               // [B][SPLIT_BINS]
     uint32_t* bin_count;         // [B][SPLIT_BINS]
     uint32_t* listed;            // [B] entries of the list, also those that it did not hold
@@ -733,65 +755,69 @@ struct SplitRow {
     }
     __device__ __forceinline__ bool by_count(int V) const { return st.top_k > 0 && st.top_k < V; }
     __device__ __forceinline__ bool by_mass() const { return st.top_p < 1.0; }
-    __device__ __forceinline__ int bin(uint32_t k) const { return bin_of(weight, k, per_bin, SPLIT_BINS); }
+    __device__ __forceinline__ int bin(float v) const { return bin_of(weight, v, per_bin, SPLIT_BINS); }
 };
 
-// the part's entries as RowKeys; index 0 of them is entry `origin` of the row
+// the part's entries as RowLogits; index 0 of them is entry `origin` of the row
 template <class T>
-__device__ __forceinline__ int split_part(const ChooseArgs& a, const SplitRows& sp, int row, int part, RowKeys<T, SPLIT_THREADS, 0>& keys) {
+__device__ __forceinline__ int split_part(const ChooseArgs& a, const SplitRows& sp, int row, int part, RowLogits<T, SPLIT_THREADS, 0>& keys) {
     const int origin = part * sp.per;
     keys.init(static_cast<const T*>(a.logits) + row * a.stride + origin, min(sp.per, a.V - origin));
+    keys.groups = sp.per / (4 * SPLIT_THREADS);                  // (of a whole part, also in a shorter last one)
+    keys.first = (int)(threadIdx.x >> 6) * keys.groups;
     return origin;
 }
 
 template <class T>
 __global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_max(ChooseArgs a, SplitRows sp) {
-    __shared__ u64 tmp[SPLIT_THREADS / 64];
+    __shared__ u64 tmp[SPLIT_THREADS / 64], tmp2[SPLIT_THREADS / 64];
     const int row = blockIdx.x / sp.parts, part = blockIdx.x - row * sp.parts, tid = threadIdx.x;
     for (int b = part * SPLIT_THREADS + tid; b < SPLIT_BINS; b += sp.parts * SPLIT_THREADS) {
         sp.bin_count[(size_t)row * SPLIT_BINS + b] = 0;
         sp.bin_mass[(size_t)row * SPLIT_BINS + b] = 0;
     }
     if (part == 0 && tid == 0) sp.listed[row] = 0;
-    RowKeys<T, SPLIT_THREADS, 0> keys;
+    RowLogits<T, SPLIT_THREADS, 0> keys;
     const int origin = split_part(a, sp, row, part, keys);
-    u64 best = 0;
-    uint32_t low = 0;
-    keys.each([&](int i, uint32_t k) { best = max(best, k ? order_key(k, origin + i) : 0), low = max(low, k ? ~k : 0u); });
-    best = block_reduce<SPLIT_THREADS>(best, tmp, OpMax{});
-    low = block_reduce<SPLIT_THREADS>(low, tmp, OpMax{});
+    u64 best;
+    uint32_t low;
+    row_ends<T, SPLIT_THREADS>(keys, origin, tmp, tmp2, best, low);
     if (tid == 0) sp.best[(size_t)row * sp.parts + part] = best, sp.low[(size_t)row * sp.parts + part] = low;
+}
+
+__device__ __forceinline__ void write_stretch(const SplitRows& sp, int row, int part, u64 sum) {
+    sum = wave_reduce(sum, OpAdd{});
+    if ((threadIdx.x & 63) == 0) sp.mass[((size_t)row * sp.parts + part) * STRETCHES + (threadIdx.x >> 6)] = sum;
 }
 
 template <class T>
 __global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_bins(ChooseArgs a, SplitRows sp, int shift) {
-    __shared__ u64 mass[SPLIT_BINS], tmp[SPLIT_THREADS / 64];
+    __shared__ u64 mass[SPLIT_BINS];
     __shared__ uint32_t count[SPLIT_BINS];
     const int row = blockIdx.x / sp.parts, part = blockIdx.x - row * sp.parts, tid = threadIdx.x;
     const SplitRow<T> r(a, sp, row, shift);
     if (r.done) return;
-    RowKeys<T, SPLIT_THREADS, 0> keys;
+    RowLogits<T, SPLIT_THREADS, 0> keys;
     split_part(a, sp, row, part, keys);
     const bool by_count = r.by_count(a.V), by_mass = r.by_mass();
     if (!by_count && !by_mass) {
         const u64 least = r.weight.least(r.st.min_p);
         u64 sum = 0;
-        keys.each([&](int, uint32_t k) {
-            const u64 w = r.weight(k);
+        keys.each([&](int, float v) {
+            const u64 w = r.weight(v);
             sum += w < least ? 0 : w;
         });
-        sum = block_reduce<SPLIT_THREADS>(sum, tmp, OpAdd{});
-        if (tid == 0) sp.mass[(size_t)row * sp.parts + part] = sum;
+        write_stretch(sp, row, part, sum);
         return;
     }
     for (int b = tid; b < SPLIT_BINS; b += SPLIT_THREADS) count[b] = 0, mass[b] = 0;
     __syncthreads();
     // (with top_k the masses are those of the list's entries)
-    keys.each([&](int, uint32_t k) {
-        if (k == 0u) return;
-        const int b = r.bin(k);
+    keys.each([&](int, float v) {
+        if (!(v > -INFINITY)) return;
+        const int b = r.bin(v);
         if (by_count) atomicAdd(&count[b], 1u);
-        else atomicAdd(&mass[b], r.weight(k));
+        else atomicAdd(&mass[b], r.weight(v));
     });
     __syncthreads();
     for (int b = tid; b < SPLIT_BINS; b += SPLIT_THREADS) {
@@ -835,20 +861,20 @@ __global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_collect(ChooseAr
     u64 missing;
     const SplitMode mode = split_cut_bin(a, sp, r, row, sh, bin, missing);
     if (mode != SPLIT_COUNT && mode != SPLIT_MASS) return;
-    RowKeys<T, SPLIT_THREADS, 0> keys;
+    RowLogits<T, SPLIT_THREADS, 0> keys;
     const int origin = split_part(a, sp, row, part, keys);
     const u64 least = r.weight.least(r.st.min_p);
     u64 sum = 0;
-    keys.each([&](int i, uint32_t k) {
-        const int b = k ? r.bin(k) : SPLIT_BINS;
+    keys.each([&](int i, float v) {
+        const int b = v > -INFINITY ? r.bin(v) : SPLIT_BINS;
         const bool take = mode == SPLIT_COUNT ? b <= bin : b == bin;
         if (mode == SPLIT_MASS && b < bin) {
-            const u64 w = r.weight(k);
+            const u64 w = r.weight(v);
             sum += w < least ? 0 : w;
         }
         if (take) {
             const uint32_t at = atomicAdd(&n_mine, 1u);
-            if (at < PART_LIST) mine[at] = order_key(k, origin + i);
+            if (at < PART_LIST) mine[at] = order_key(logit_key<T>(v), origin + i);
         }
     });
     __syncthreads();
@@ -860,16 +886,13 @@ __global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_collect(ChooseAr
         for (uint32_t i = tid; i < min(n, (uint32_t)PART_LIST); i += SPLIT_THREADS)
             if (base + i < LIST) sp.list[(size_t)row * LIST + base + i] = mine[i];
     }
-    if (mode == SPLIT_MASS) {
-        sum = block_reduce<SPLIT_THREADS>(sum, sh.tmp, OpAdd{});
-        if (tid == 0) sp.mass[(size_t)row * sp.parts + part] = sum;
-    }
+    if (mode == SPLIT_MASS) write_stretch(sp, row, part, sum);
 }
 
 template <class T>
 __global__ __launch_bounds__(FINISH_THREADS) void k_choose_split_finish(ChooseArgs a, SplitRows sp, int shift) {
     __shared__ ChooseShared<FINISH_THREADS> sh;
-    __shared__ u64 list[LIST], part_mass[SPLIT_PARTS];
+    __shared__ u64 list[LIST], stretch[SPLIT_PARTS * STRETCHES];
     const int row = blockIdx.x, tid = threadIdx.x;
     const SplitRow<T> r(a, sp, row, shift);
     if (r.done) {
@@ -883,11 +906,14 @@ __global__ __launch_bounds__(FINISH_THREADS) void k_choose_split_finish(ChooseAr
         return;
     }
     for (uint32_t i = tid; i < listed; i += FINISH_THREADS) list[i] = sp.list[(size_t)row * LIST + i];
-    if (tid < SPLIT_PARTS) part_mass[tid] = !by_count && tid < sp.parts ? sp.mass[(size_t)row * sp.parts + tid] : 0;
+    const int stretches = sp.parts * STRETCHES, wide = sp.per / STRETCHES;
+    for (int i = tid; i < SPLIT_PARTS * STRETCHES; i += FINISH_THREADS)
+        stretch[i] = !by_count && i < stretches ? sp.mass[(size_t)row * stretches + i] : 0;
     __syncthreads();
     const u64 least = r.weight.least(r.st.min_p);
     u64 cut = 1ull << 32;
-    auto weight = [&](u64 o) { return r.weight((uint32_t)(o >> 32)); };
+    auto logit = [&](u64 o) { return key_logit<T>((uint32_t)(o >> 32)); };
+    auto weight = [&](u64 o) { return r.weight(logit(o)); };
     auto kept = [&](u64 o) {
         const u64 w = o < cut ? 0 : weight(o);
         return w < least ? (u64)0 : w;
@@ -914,13 +940,13 @@ __global__ __launch_bounds__(FINISH_THREADS) void k_choose_split_finish(ChooseAr
         const u64 at = find_entry<FINISH_THREADS>(entries([](u64 o) { return o & 0xffffffffull; }, kept), target + 1, sh);
         for (uint32_t i = tid; i < listed; i += FINISH_THREADS)
             if ((list[i] & 0xffffffffull) == at)
-                write_choice(a, row, (int)~(uint32_t)at, r.weight.log_share((uint32_t)(list[i] >> 32), total));
+                write_choice(a, row, (int)~(uint32_t)at, r.weight.log_share(logit(list[i]), total));
         return;
     }
     if (by_mass) {
         // what is missing of the mass in the list's bin: the bins before it hold the rest
         u64 total = 0, before = 0;
-        const int bin = r.bin((uint32_t)(list[0] >> 32));
+        const int bin = r.bin(logit(list[0]));
         for (int b = tid; b < SPLIT_BINS; b += FINISH_THREADS) {
             const u64 v = sp.bin_mass[(size_t)row * SPLIT_BINS + b];
             total += v;
@@ -931,23 +957,25 @@ __global__ __launch_bounds__(FINISH_THREADS) void k_choose_split_finish(ChooseAr
         cut = find_entry<FINISH_THREADS>(entries(order, weight), mass_of(r.st.top_p, total) - before, sh);
         for (uint32_t i = tid; i < listed; i += FINISH_THREADS) {
             const u64 w = kept(list[i]);
-            if (w) atomicAdd(&part_mass[~(uint32_t)list[i] / (uint32_t)sp.per], w);
+            if (w) atomicAdd(&stretch[~(uint32_t)list[i] / (uint32_t)wide], w);
         }
         __syncthreads();
     }
-    // the part in which the running sum exceeds the target
-    const int lane = tid & 63;
-    const u64 mine = part_mass[lane], run = wave_scan(mine, OpAdd{}), total = lane_value(run, 63), target = target_of(r.st.u, total);
-    const int part = __ffsll(__ballot(run > target)) - 1;
-    const u64 start = lane_value(run - mine, part);
-    RowKeys<T, FINISH_THREADS, 0> keys;
-    const int origin = part * sp.per;
-    keys.init(static_cast<const T*>(a.logits) + row * a.stride + origin, min(sp.per, a.V - origin));
-    auto kept_at = [&](int i, uint32_t k) { return k ? kept(order_key(k, origin + i)) : (u64)0; };
-    u64 sum = 0, part_total;
-    keys.each([&](int i, uint32_t k) { sum += kept_at(i, k); });
+    // the stretch in which the running sum exceeds the target
+    static_assert(SPLIT_PARTS * STRETCHES == FINISH_THREADS, "a stretch to a thread");
+    u64 total;
+    const u64 mine = stretch[tid], run = block_scan<FINISH_THREADS>(mine, sh.tmp, total), target = target_of(r.st.u, total);
+    if (run - mine <= target && target < run) sh.found[0] = tid, sh.found[1] = run - mine;
+    __syncthreads();
+    const int origin = (int)sh.found[0] * wide, lane = tid & 63;
+    const u64 start = sh.found[1];
+    RowLogits<T, FINISH_THREADS, 0> keys;
+    keys.init(static_cast<const T*>(a.logits) + row * a.stride + origin, min(wide, a.V - origin));
+    auto kept_at = [&](int i, float v) { return v > -INFINITY ? kept(order_key(logit_key<T>(v), origin + i)) : (u64)0; };
+    u64 sum = 0, all;
+    keys.each([&](int i, float v) { sum += kept_at(i, v); });
     const u64 wave_sum = wave_reduce(sum, OpAdd{});
-    const u64 end = lane_value(block_scan<FINISH_THREADS>(lane == 63 ? wave_sum : 0, sh.tmp, part_total), 63);
+    const u64 end = lane_value(block_scan<FINISH_THREADS>(lane == 63 ? wave_sum : 0, sh.tmp, all), 63);
     choose_among(a, row, keys, origin, start, target, total, wave_sum, end, r.weight, kept_at);
 }
 
@@ -965,7 +993,8 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 size_t split_layout(int B, int V, char* p, SplitRows& sp) {
     sp.parts = split_parts(B, V);
     if (sp.parts == 0) return 0;
-    sp.per = ((V + sp.parts - 1) / sp.parts + 3) & ~3;
+    sp.per = ((V + sp.parts - 1) / sp.parts + 4 * SPLIT_THREADS - 1) / (4 * SPLIT_THREADS) * (4 * SPLIT_THREADS);
+    sp.parts = (V + sp.per - 1) / sp.per;
     size_t n = 0;
     auto take = [&](auto*& field, size_t count) {
         field = reinterpret_cast<std::remove_reference_t<decltype(field)>>(p + n);
@@ -973,7 +1002,7 @@ size_t split_layout(int B, int V, char* p, SplitRows& sp) {
     };
     take(sp.best, (size_t)B * sp.parts);
     take(sp.low, (size_t)B * sp.parts);
-    take(sp.mass, (size_t)B * sp.parts);
+    take(sp.mass, (size_t)B * sp.parts * STRETCHES);
     take(sp.bin_mass, (size_t)B * SPLIT_BINS);
     take(sp.bin_count, (size_t)B * SPLIT_BINS);
     take(sp.listed, (size_t)B);
@@ -992,6 +1021,7 @@ void launch_choose_rows(const ChooseArgs& a, int shift, hipStream_t s) {
     else if (V <= 512) hipLaunchKernelGGL((k_choose_wave<T, 4, 2>), waves, dim3(256), 0, s, a, shift);
     else if (V <= 1024) hipLaunchKernelGGL((k_choose_wave<T, 4, 4>), waves, dim3(256), 0, s, a, shift);
     else if (V <= 2048) hipLaunchKernelGGL((k_choose_block<T, 256, 2>), rows, dim3(256), 0, s, a, shift);
+    else if (V <= 4096) hipLaunchKernelGGL((k_choose_block<T, 512, 2>), rows, dim3(512), 0, s, a, shift);
     else if (V <= 8192) hipLaunchKernelGGL((k_choose_block<T, 1024, 2>), rows, dim3(1024), 0, s, a, shift);
     else if (split_layout(a.B, V, static_cast<char*>(a.workspace), sp) == 0)
         hipLaunchKernelGGL((k_choose_block<T, 1024, 0>), rows, dim3(1024), 0, s, a, shift);
@@ -1012,11 +1042,14 @@ size_t choose_workspace(int B, int V) {
     return B > 0 ? split_layout(B, V, nullptr, sp) : 0;
 }
 
-void launch_choose(const ChooseArgs& a, hipStream_t s) {
-    if (a.B == 0) return;
+void launch_choose(const ChooseArgs& args, hipStream_t s) {
+    if (args.B == 0) return;
     int log_v = 0;
-    while (((int64_t)1 << log_v) < a.V) ++log_v;
+    while (((int64_t)1 << log_v) < args.V) ++log_v;
     const int shift = 61 - log_v;
+    ChooseArgs a = args;
+    a.inv_t = 1.f / a.temperature.v;
+    a.log2e_t = 1.4426950408889634074 / (double)a.temperature.v;
     if (a.type == ROW_FLOAT32) launch_choose_rows<float>(a, shift, s);
     else if (a.type == ROW_BFLOAT16) launch_choose_rows<__bf16>(a, shift, s);
     else launch_choose_rows<_Float16>(a, shift, s);

@@ -58,6 +58,8 @@ struct ChooseArgs {
     int32_t* index;
     float* logq;              // or nullptr
     void* workspace;
+    float inv_t;              // 1 / T and log2(e) / T where T holds for all rows: filled in by launch_choose
+    double log2e_t;
 };
 size_t choose_workspace(int B, int V);
 void launch_choose(const ChooseArgs& a, hipStream_t s);
