@@ -707,8 +707,8 @@ __global__ __launch_bounds__(NT, 4) void k_choose_block(ChooseArgs a, int shift)
 
 // ------------------------------------------------------------------------------------ several workgroups for every row
 //
-// Few long rows: `parts` workgroups of SPLIT_THREADS for every row, each with a stretch of `per` entries, in four launches
-// (three where no filter is on).
+// Long rows: `parts` workgroups of SPLIT_THREADS for every row, each with a stretch of `per` entries, in four launches (three
+// where no filter is on) for every batch of SPLIT_ROWS rows.
 //   max      the largest order key of every part
 //   bins     the row's histogram over the distance from the largest logit, summed up by integer atomics (exact, in any
 //            order); rows without top_k and top_p: the kept mass of every part instead
@@ -979,19 +979,20 @@ __global__ __launch_bounds__(FINISH_THREADS) void k_choose_split_finish(ChooseAr
     choose_among(a, row, keys, origin, start, target, total, wave_sum, end, r.weight, kept_at);
 }
 
-// Parts of a row, 0 for rows that are not split: those of more than 8192 entries (up to there a workgroup keeps the keys in
-// its registers), as long as there are few enough rows to leave workgroups for it.
-constexpr int SPLIT_WORKGROUPS = 1024;
+// Parts of a row, 0 for rows that a workgroup does alone: up to 4096 entries, and up to 8192 (it keeps their logits in its
+// registers) as long as all rows run at once, two to a compute unit.  Measured with all filters, us, alone and split: 64 rows
+// of 8000 26 and 29, 1000 of 8000 95 and 51, 300 of 25000 101 and 39, 500 of 16384 75 and 38.
+constexpr int SPLIT_WORKGROUPS = 1024, SPLIT_ROWS = 1024;        // in a batch of rows; rows of a batch
 int split_parts(int B, int V) {
-    if (V <= 8192 || B > SPLIT_WORKGROUPS / 4) return 0;
-    const int parts = min((V + 4095) / 4096, SPLIT_WORKGROUPS / B);
-    return min(max(parts, 1), SPLIT_PARTS);
+    if (V <= 4096 || (V <= 8192 && B <= 2 * EINET_NUM_CUS)) return 0;
+    return min(min((V + 4095) / 4096, max(2, SPLIT_WORKGROUPS / B)), SPLIT_PARTS);
 }
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
-// lays the workspace out; p == nullptr: its size alone
+// lays the workspace of a batch out; p == nullptr: its size alone
 size_t split_layout(int B, int V, char* p, SplitRows& sp) {
     sp.parts = split_parts(B, V);
+    B = min(B, SPLIT_ROWS);
     if (sp.parts == 0) return 0;
     sp.per = ((V + sp.parts - 1) / sp.parts + 4 * SPLIT_THREADS - 1) / (4 * SPLIT_THREADS) * (4 * SPLIT_THREADS);
     sp.parts = (V + sp.per - 1) / sp.per;
@@ -1010,6 +1011,32 @@ size_t split_layout(int B, int V, char* p, SplitRows& sp) {
     return n;
 }
 
+// the call for rows b0 .. b0 + n - 1
+ChooseArgs rows_from(const ChooseArgs& a, int b0, int n) {
+    ChooseArgs r = a;
+    r.B = n;
+    r.logits = static_cast<const char*>(a.logits) + (int64_t)b0 * a.stride * row_type_bytes(a.type);
+    r.u += b0;
+    r.index += b0;
+    if (a.logq) r.logq += b0;
+    if (a.temperature.p) r.temperature.p += b0;
+    if (a.top_k.p) r.top_k.p += b0;
+    if (a.top_p.p) r.top_p.p += b0;
+    if (a.min_p.p) r.min_p.p += b0;
+    return r;
+}
+
+template <class T>
+void launch_choose_split(const ChooseArgs& a, const SplitRows& sp, int shift, hipStream_t s) {
+    const dim3 parts(a.B * sp.parts), rows(a.B);
+    hipLaunchKernelGGL(k_choose_split_max<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp);
+    const bool weighted = a.temperature.p || a.temperature.v > 0.f;          // (else the largest entry it is)
+    if (weighted) hipLaunchKernelGGL(k_choose_split_bins<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp, shift);
+    const bool filters = a.top_k.p || a.top_p.p || (a.top_k.v > 0 && a.top_k.v < a.V) || a.top_p.v < 1.f;
+    if (weighted && filters) hipLaunchKernelGGL(k_choose_split_collect<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp, shift);
+    hipLaunchKernelGGL(k_choose_split_finish<T>, rows, dim3(FINISH_THREADS), 0, s, a, sp, shift);
+}
+
 template <class T>
 void launch_choose_rows(const ChooseArgs& a, int shift, hipStream_t s) {
     const int V = a.V;
@@ -1022,17 +1049,10 @@ void launch_choose_rows(const ChooseArgs& a, int shift, hipStream_t s) {
     else if (V <= 1024) hipLaunchKernelGGL((k_choose_wave<T, 4, 4>), waves, dim3(256), 0, s, a, shift);
     else if (V <= 2048) hipLaunchKernelGGL((k_choose_block<T, 256, 2>), rows, dim3(256), 0, s, a, shift);
     else if (V <= 4096) hipLaunchKernelGGL((k_choose_block<T, 512, 2>), rows, dim3(512), 0, s, a, shift);
-    else if (V <= 8192) hipLaunchKernelGGL((k_choose_block<T, 1024, 2>), rows, dim3(1024), 0, s, a, shift);
     else if (split_layout(a.B, V, static_cast<char*>(a.workspace), sp) == 0)
-        hipLaunchKernelGGL((k_choose_block<T, 1024, 0>), rows, dim3(1024), 0, s, a, shift);
-    else {
-        const dim3 parts(a.B * sp.parts);
-        hipLaunchKernelGGL(k_choose_split_max<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp);
-        hipLaunchKernelGGL(k_choose_split_bins<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp, shift);
-        const bool filters = a.top_k.p || a.top_p.p || (a.top_k.v > 0 && a.top_k.v < V) || a.top_p.v < 1.f;
-        if (filters) hipLaunchKernelGGL(k_choose_split_collect<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp, shift);
-        hipLaunchKernelGGL(k_choose_split_finish<T>, rows, dim3(FINISH_THREADS), 0, s, a, sp, shift);
-    }
+        hipLaunchKernelGGL((k_choose_block<T, 1024, 2>), rows, dim3(1024), 0, s, a, shift);
+    else
+        for (int b0 = 0; b0 < a.B; b0 += SPLIT_ROWS) launch_choose_split<T>(rows_from(a, b0, min(a.B - b0, SPLIT_ROWS)), sp, shift, s);
 }
 
 }  // namespace

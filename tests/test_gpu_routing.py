@@ -358,6 +358,27 @@ def test_choose_rows_in_wider_rows_and_the_same_row_for_all():
     assert P.einet_choose(torch.zeros(0, 9, device="cuda"), torch.zeros(0, device="cuda"))[0].shape == (0,)
 
 
+@pytest.mark.parametrize("B,V", [(1100, 4100), (600, 8192), (2100, 5000), (1025, 20000)])
+def test_choose_from_many_long_rows(B, V):
+    """Rows enough for several batches: the same choices as from the rows alone, and the oracle's for some of them."""
+    rng = np.random.default_rng(B)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(B)
+    x = torch.randn(B, V, generator=g, device="cuda") * 3
+    u = uniforms(rng, B)
+    t, k, p, m = (torch.rand(B, generator=g, device="cuda") for _ in range(4))
+    settings = dict(temperature=t + 0.3, top_k=(k * 90).int(), top_p=0.5 + 0.6 * p, min_p=0.1 * m)
+    for use in (dict(), dict(top_p=0.9), settings):
+        print("choose", B, V, list(use), flush=True)
+        index, logq = P.einet_choose(x, u, **use)
+        for lo, hi in ((0, 9), (1020, 1030), (B - 7, B)):
+            part = {k: v[lo:hi].contiguous() if torch.is_tensor(v) else v for k, v in use.items()}
+            i, q = P.einet_choose(x[lo:hi], u[lo:hi].contiguous(), **part)
+            assert torch.equal(i, index[lo:hi]) and torch.equal(q, logq[lo:hi])
+        last = {k: v[B - 2:].contiguous() if torch.is_tensor(v) else v for k, v in use.items()}
+        assert torch.equal(check_choose(x[B - 2:], u[B - 2:].contiguous(), **last), index[B - 2:])
+
+
 def test_choices_have_the_frequencies_of_the_kept_distribution():
     n = 200000
     logits = torch.log(torch.tensor([0.05, 0.3, 0.15, 0.5], device="cuda"))
