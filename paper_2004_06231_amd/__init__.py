@@ -11,3 +11,4 @@ from .binding import (EiNet, EinetError, load_library, LIB_PATH,  # noqa: F401
                       einet_mixture_logp, einet_sample, einet_last_error, einet_profile_enable, einet_profile_read, measure_peaks,
                       einet_route, einet_route_backward, einet_sort, einet_dispatch, einet_combine, einet_combine_backward, einet_choose,
                       BERNOULLI, GAUSSIAN, BINOMIAL, CATEGORICAL, EXPORTED_SYMBOLS)
+from .mixture import Mixture  # noqa: F401

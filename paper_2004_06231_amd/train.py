@@ -6,12 +6,15 @@ mini-batch EM (Eq. 8-9: batch 500, step 0.5, variances kept in [1e-6, 1e-2]); th
 cluster proportions.  The components are independent, so their epochs are enqueued round-robin on several HIP
 streams of equal priority: one small circuit does not fill the chip, several side by side do.  With --graphs
 every component's epoch (the same launches on the same buffers every time) is captured into a HIP graph after
-the first epoch and replayed from then on, which takes the host's launch calls out of the loop.  Prints one
-JSON line: training throughput over all epochs and over the epochs after the first (which also loads the
+the first epoch and replayed from then on, which takes the host's launch calls out of the loop.  With --reassign
+the clusters of the synthetic data hold for the first epoch only: before every later one all samples are routed
+anew, each to its most probable component (best) or to one drawn from its posterior (draw), and the coefficients
+follow.  Prints one JSON line: training throughput over all epochs and over the epochs after the first (which also loads the
 kernels), seconds per epoch, mean training logP of each epoch (first component) and the mean mixture logP of
 a held-out batch.
 
     python -m paper_2004_06231_amd.train --shape svhn --components 8 --epochs 3 --n 5000 --streams 4 --graphs
+    python -m paper_2004_06231_amd.train --shape svhn --components 8 --epochs 5 --n 5000 --streams 4 --reassign best
 """
 import argparse
 import json
@@ -33,7 +36,11 @@ def main():
     ap.add_argument("--streams", type=int, default=4)
     ap.add_argument("--seed", type=int, default=42)
     ap.add_argument("--graphs", action="store_true", help="replay a captured HIP graph per component after the first epoch")
+    ap.add_argument("--reassign", default="never", choices=["never", "best", "draw"],
+                    help="route all samples to components anew before every epoch after the first")
     args = ap.parse_args()
+    if args.graphs and args.reassign != "never":
+        ap.error("--graphs replays the same batches every epoch: it does not go with --reassign")
     cfg = workloads.sec42_config(args.shape)
     K, C, fam, B = cfg["K"], cfg["channels"], cfg["family"], cfg["B"]
     models, data, lps = [], [], []
@@ -73,17 +80,35 @@ def main():
             with torch.cuda.stream(streams[c % len(streams)]):
                 g.replay()
 
+    log_coef = torch.as_tensor(np.log(sizes / sizes.sum()), dtype=torch.float32).cuda()
+    mixture = pooled = ids = None
+    if args.reassign != "never":
+        mixture = P.Mixture(models, log_coef, streams)
+        pooled = torch.cat(data)
+        ids = torch.repeat_interleave(torch.arange(len(models), dtype=torch.int32), torch.as_tensor(sizes)).cuda()
+        torch.manual_seed(args.seed)
+    moved = []
+
+    def routed_epoch(ids):
+        u = torch.rand(pooled.shape[0], device="cuda") if args.reassign == "draw" else None
+        now, lp = mixture.em_epoch(pooled, None, batch=B, u=u, **cfg["em"])
+        moved.append(int((now != ids).sum()))
+        return now, lp
+
     history, seconds = [], []
     t0 = time.perf_counter()
     for e in range(args.epochs):
         t1 = time.perf_counter()
         if graphs:
             replay()
+        elif mixture is not None and e > 0:
+            ids, lp = routed_epoch(ids)
         else:
             epoch()
         torch.cuda.synchronize()
         seconds.append(round(time.perf_counter() - t1, 4))
-        history.append(round(float(lps[0].mean()), 3))
+        first = lps[0] if mixture is None or e == 0 else lp[ids == 0]
+        history.append(round(float(first.mean()), 3))
         if args.graphs and e == 0 and args.epochs > 1:
             capture()                                    # (its time counts in the total, not in an epoch's)
     dt = time.perf_counter() - t0
@@ -91,8 +116,7 @@ def main():
     rows = torch.empty(args.components, held_out.shape[0], dtype=torch.float32, device="cuda")
     for c, m in enumerate(models):
         m.logp(held_out, None, rows[c])
-    log_coef = torch.as_tensor(np.log(sizes / sizes.sum()), dtype=torch.float32).cuda()
-    mix = P.einet_mixture_logp(rows, log_coef)
+    mix = P.einet_mixture_logp(rows, log_coef if mixture is None else mixture.log_coef)
     assert bool(torch.isfinite(mix).all()) and all(bool(torch.isfinite(m.params).all()) for m in models)
     total = int(sizes.sum()) * args.epochs
     later = sum(seconds[1:])
@@ -102,7 +126,8 @@ def main():
                           train_samples_per_s=round(total / dt, 1), seconds=round(dt, 4), seconds_per_epoch=seconds,
                           samples_per_s_after_first_epoch=round(int(sizes.sum()) * (args.epochs - 1) / later, 1) if later > 0 else None,
                           train_mean_logp_per_epoch_component0=history,
-                          held_out_mixture_mean_logp=round(float(mix.mean()), 3))))
+                          held_out_mixture_mean_logp=round(float(mix.mean()), 3),
+                          **({} if mixture is None else dict(reassign=args.reassign, samples_moved_per_epoch=moved)))))
     for m in models:
         m.close()
 
