@@ -341,7 +341,7 @@ int einet_route(const void* score_dev, int dtype, int64_t component_stride, int6
                 const float* log_coef_dev, int n_components, int64_t n, int top, int renormalise, int32_t* id_dev,
                 float* weight_dev, float* logp_dev, void* stream);
 
-/* Bytes of device workspace that einet_route_backward needs for dlog_coef_dev.  bytes: host. */
+/* Bytes of device workspace that einet_route_backward needs for dlog_coef_dev (0 is possible).  bytes: host. */
 int einet_route_workspace(int n_components, int64_t n, size_t* bytes);
 
 /* Gradient of einet_route: from dweight = dL/dweight and dlogp = dL/dlogp the gradients of the scores and of the log
@@ -352,7 +352,7 @@ int einet_route_workspace(int n_components, int64_t n, size_t* bytes);
  *   dlogp_dev      device, [n] float32, or NULL
  *   dscore_dev     device, written completely, of `dtype`, entry (c, i) at c * dcomponent_stride + i * dsample_stride
  *   dlog_coef_dev  device, [n_components] float32, written, or NULL; needs the workspace (einet_route_workspace bytes,
- *                  16-byte aligned)
+ *                  16-byte aligned; NULL if that is 0)
  * The entries of dscore_dev must share no memory with each other nor with an input.  n = 0 writes zeros to dlog_coef_dev.  Errors as einet_route. */
 int einet_route_backward(const void* score_dev, int dtype, int64_t component_stride, int64_t sample_stride,
                          const float* log_coef_dev, int n_components, int64_t n, int top, int renormalise,

@@ -433,14 +433,15 @@ def _row_type(t):
     if not _ROW_TYPES:
         import torch
         _ROW_TYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
-    assert t.dtype in _ROW_TYPES, f"float32, bfloat16 or float16 is needed, got {t.dtype}"
-    return _ROW_TYPES[t.dtype]
+    number = _ROW_TYPES.get(t.dtype)
+    assert number is not None, f"float32, bfloat16 or float16 is needed, got {t.dtype}"
+    return number
 
 
 def _on(device, dtype, shape, *tensors):
     """The C ABI sees pointers only: every tensor must be a contiguous one of this type and shape on this device."""
     for t in tensors:
-        assert t is None or (t.dtype == dtype and t.device == device and tuple(t.shape) == tuple(shape) and t.is_contiguous()), \
+        assert t is None or (t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous()), \
             f"a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is needed, got {t.dtype} {tuple(t.shape)} on {t.device}"
 
 
@@ -536,12 +537,15 @@ def einet_sort(ids, n_components):
 def _rows(t, what):
     """(rows, width, stride between rows) of a tensor whose rows are dense."""
     assert t.is_cuda and t.dim() >= 2, f"{what} must be a cuda tensor of rows"
-    width, want = 1, 1
-    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+    shape = t.shape
+    n, width = shape[0], shape[1] if t.dim() == 2 else math.prod(shape[1:])
+    if t.is_contiguous():
+        return n, width, width
+    want = 1
+    for size, stride in zip(reversed(shape[1:]), reversed(t.stride()[1:])):
         assert size <= 1 or stride == want, f"every row of {what} must be contiguous"
         want *= size
-        width *= size
-    return t.shape[0], width, t.stride(0) if t.shape[0] > 1 else width
+    return n, width, t.stride(0) if n > 1 else width
 
 
 def _slots(place, n, device):
@@ -559,9 +563,11 @@ def einet_dispatch(x, place, out=None):
     n, width, stride = _rows(x, "x")
     top = _slots(place, n, x.device)
     if out is None:
-        out = torch.empty((n * top,) + tuple(x.shape[1:]), dtype=x.dtype, device=x.device)
-    assert out.dtype == x.dtype and out.device == x.device and out.shape[1:] == x.shape[1:]
-    rows, _, out_stride = _rows(out, "out")
+        out = x.new_empty((n * top,) + x.shape[1:])
+        rows, out_stride = n * top, width
+    else:
+        assert out.dtype is x.dtype and out.device == x.device and out.shape[1:] == x.shape[1:]
+        rows, _, out_stride = _rows(out, "out")
     e = x.element_size()
     _enqueue("einet_dispatch", x.device, x.data_ptr(), width * e, stride * e, n, top, place.data_ptr(), out.data_ptr(),
              out_stride * e, rows)
@@ -577,9 +583,11 @@ def einet_combine(rows, place, weights=None, out=None):
     top = _slots(place, n, rows.device)
     _on(rows.device, torch.float32, place.shape, weights)
     if out is None:
-        out = torch.empty((n,) + tuple(rows.shape[1:]), dtype=rows.dtype, device=rows.device)
-    assert out.dtype == rows.dtype and out.device == rows.device and out.shape[1:] == rows.shape[1:] and out.shape[0] == n
-    out_stride = _rows(out, "out")[2]
+        out = rows.new_empty((n,) + rows.shape[1:])
+        out_stride = width
+    else:
+        assert out.dtype is rows.dtype and out.device == rows.device and out.shape[1:] == rows.shape[1:] and out.shape[0] == n
+        out_stride = _rows(out, "out")[2]
     _enqueue("einet_combine", rows.device, rows.data_ptr(), _row_type(rows), width, stride, m, place.data_ptr(), _ptr(weights), n,
              top, out.data_ptr(), out_stride)
     return out
@@ -593,12 +601,14 @@ def einet_combine_backward(dout, rows, place, weights, out=None):
     n = place.shape[0]
     top = _slots(place, n, rows.device)
     _on(rows.device, torch.float32, place.shape, weights)
-    assert dout.dtype == rows.dtype and dout.device == rows.device and tuple(dout.shape) == (n,) + tuple(rows.shape[1:])
+    assert dout.dtype is rows.dtype and dout.device == rows.device and dout.shape == (n,) + rows.shape[1:]
     dout_stride = _rows(dout, "dout")[2]
     if out is None:
-        out = torch.empty(tuple(rows.shape), dtype=rows.dtype, device=rows.device)
-    assert out.dtype == rows.dtype and out.device == rows.device and out.shape == rows.shape
-    out_stride = _rows(out, "out")[2]
+        out = rows.new_empty(rows.shape)
+        out_stride = width
+    else:
+        assert out.dtype is rows.dtype and out.device == rows.device and out.shape == rows.shape
+        out_stride = _rows(out, "out")[2]
     dweights = torch.empty(place.shape, dtype=torch.float32, device=rows.device)
     _enqueue("einet_combine_backward", rows.device, dout.data_ptr(), dout_stride, rows.data_ptr(), _row_type(rows), width, stride, m,
              place.data_ptr(), weights.data_ptr(), n, top, out.data_ptr(), out_stride, dweights.data_ptr())

@@ -85,7 +85,7 @@ int einet_route_backward(const void* score_dev, int dtype, int64_t component_str
         !aligned(dlogp_dev, 4) || !aligned(dlog_coef_dev, 4))
         return invalid(call, "a pointer is not aligned to its elements");
     const size_t need = route_backward_workspace(n_components, n);
-    if (dlog_coef_dev && n > 0 && (!workspace_dev || !aligned(workspace_dev, 16) || workspace_bytes < need))
+    if (dlog_coef_dev && need > 0 && (!workspace_dev || !aligned(workspace_dev, 16) || workspace_bytes < need))
         return invalid(call, "dlog_coef_dev needs a workspace of einet_route_workspace bytes, 16-byte aligned");
     launch_route_backward(Scores{score_dev, dtype, component_stride, sample_stride, log_coef_dev, n_components, n}, top,
                           renormalise != 0, id_dev, weight_dev, dweight_dev, dlogp_dev, dscore_dev, dcomponent_stride,

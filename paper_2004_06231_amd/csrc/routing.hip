@@ -412,8 +412,10 @@ int route_lanes(int M, int top) {
 // compute unit to have two workgroups' worth of lanes.
 bool route_by_columns(const Scores& a, int top) { return a.sn == 1 && a.M <= ROUTE_COLUMNS_MOST && top <= 4 && a.N >= 2 * 256 * EINET_NUM_CUS; }
 
-// Workgroups of the gradient, which is the rows of its workspace.
-int route_backward_groups(int64_t N) {
+// Workgroups of the gradient, which is the rows of its workspace.  A handful of samples are one workgroup's, whose sums are
+// the gradient of the coefficients: no second launch and no workspace.
+int route_backward_groups(int M, int64_t N) {
+    if (N <= (M <= 64 ? 32 : 8)) return 1;
     const int64_t tiles = (N + 3) / 4;               // (a workgroup has four samples at least)
     return (int)(tiles < 2 * EINET_NUM_CUS ? tiles : 2 * EINET_NUM_CUS);
 }
@@ -562,8 +564,9 @@ __global__ __launch_bounds__(64 * SORT_WAVES) void k_sort(const int32_t* __restr
 // ------------------------------------------------------------------------------------------- rows there and back
 //
 // A row is a number of units of up to 16 bytes (the last may be shorter; loads and stores of 16 bytes need no more than the
-// elements' alignment).  L lanes share a sample, each with UN units of every L * UN: a tile.  A tile's work is one item, so
-// that a few long rows spread over many workgroups too; rows shorter than half a wave's units share a wave.
+// elements' alignment).  L lanes share a sample, each with one unit of every L: a tile.  A tile's work is one item, so that
+// a few long rows spread over many workgroups too; rows shorter than half a wave's units share a wave.  (Two units to a lane
+// of longer rows: 8192 samples with four rows of 2048 bf16 each way, with gradients, 187 us instead of 181, four 193.)
 template <class T> constexpr int UNIT = 16 / (int)sizeof(T);
 template <class T> struct Unit { T v[UNIT<T>]; };
 
@@ -586,55 +589,42 @@ __device__ __forceinline__ void store_unit(T* p, int64_t left, const Unit<T>& u)
         if (i < left) p[i] = u.v[i];
 }
 
-// The item of a lane: its sample and the column of its first unit.
-template <class T, int L, int UN>
-__device__ __forceinline__ bool row_item(int64_t N, int tiles, int64_t& n, int64_t& k0) {
-    uint32_t item = blockIdx.x * (256 / L) + threadIdx.x / L;        // (N * tiles < 2^32: checked by the launcher)
+// The item of a lane: its sample and the column of its unit.
+template <class T, int L>
+__device__ __forceinline__ bool row_item(int64_t N, int64_t H, int tiles, int64_t& n, int64_t& k) {
+    uint32_t item = blockIdx.x * (256 / L) + threadIdx.x / L;        // (N * tiles < 2^31: seen to by the launcher)
     if constexpr (L == 64) item = (uint32_t)__builtin_amdgcn_readfirstlane((int)item);
     const uint32_t i = tiles == 1 ? item : item / (uint32_t)tiles;
     n = i;
-    k0 = ((int64_t)(item - i * (uint32_t)tiles) * (L * UN) + threadIdx.x % L) * UNIT<T>;
-    return n < N;
+    k = ((int64_t)(item - i * (uint32_t)tiles) * L + threadIdx.x % L) * UNIT<T>;
+    return n < N && k < H;
 }
 
-template <class T, int L, int UN>
+template <class T, int L>
 __global__ __launch_bounds__(256) void k_dispatch(const T* __restrict__ x, int64_t H, int64_t x_stride, int64_t N, int tiles, int top,
                                                   const int32_t* __restrict__ place, T* __restrict__ out, int64_t out_stride,
                                                   int64_t out_rows) {
-    int64_t n, k0;
-    if (!row_item<T, L, UN>(N, tiles, n, k0)) return;
-    Unit<T> u[UN];
-#pragma unroll
-    for (int i = 0; i < UN; ++i) {
-        const int64_t k = k0 + i * L * UNIT<T>;
-        if (k < H) u[i] = load_unit(x + n * x_stride + k, H - k);
-    }
+    int64_t n, k;
+    if (!row_item<T, L>(N, H, tiles, n, k)) return;
+    const Unit<T> u = load_unit(x + n * x_stride + k, H - k);
     for (int s = 0; s < top; ++s) {
         const int64_t at = place[n * top + s];
-        if (at < 0 || at >= out_rows) continue;
-        T* const row = out + at * out_stride;
-#pragma unroll
-        for (int i = 0; i < UN; ++i) {
-            const int64_t k = k0 + i * L * UNIT<T>;
-            if (k < H) store_unit(row + k, H - k, u[i]);
-        }
+        if (at >= 0 && at < out_rows) store_unit(out + at * out_stride + k, H - k, u);
     }
 }
 
 // Slots are taken S at a time, their loads in flight together.
-template <class T, int L, int UN, int S>
+template <class T, int L, int S>
 __global__ __launch_bounds__(256) void k_combine(const T* __restrict__ rows, int64_t H, int64_t stride, int64_t n_rows,
                                                  const int32_t* __restrict__ place, const float* __restrict__ weights, int64_t N,
                                                  int tiles, int top, T* __restrict__ out, int64_t out_stride) {
-    int64_t n, k0;
-    if (!row_item<T, L, UN>(N, tiles, n, k0)) return;
-    float acc[UN][UNIT<T>];
+    int64_t n, k;
+    if (!row_item<T, L>(N, H, tiles, n, k)) return;
+    float acc[UNIT<T>];
 #pragma unroll
-    for (int i = 0; i < UN; ++i)
-#pragma unroll
-        for (int c = 0; c < UNIT<T>; ++c) acc[i][c] = 0.f;
+    for (int c = 0; c < UNIT<T>; ++c) acc[c] = 0.f;
     for (int s0 = 0; s0 < top; s0 += S) {
-        Unit<T> u[S][UN];
+        Unit<T> u[S];
         float w[S];
         bool has[S];
 #pragma unroll
@@ -643,31 +633,19 @@ __global__ __launch_bounds__(256) void k_combine(const T* __restrict__ rows, int
             const int64_t at = place[slot];
             has[q] = s0 + q < top && at >= 0 && at < n_rows;
             w[q] = weights ? weights[slot] : 1.f;
-            if (has[q]) {
-#pragma unroll
-                for (int i = 0; i < UN; ++i) {
-                    const int64_t k = k0 + i * L * UNIT<T>;
-                    if (k < H) u[q][i] = load_unit(rows + at * stride + k, H - k);
-                }
-            }
+            if (has[q]) u[q] = load_unit(rows + at * stride + k, H - k);
         }
 #pragma unroll
         for (int q = 0; q < S; ++q)
             if (has[q]) {
 #pragma unroll
-                for (int i = 0; i < UN; ++i)
-#pragma unroll
-                    for (int c = 0; c < UNIT<T>; ++c) acc[i][c] = fmaf(w[q], to_float(u[q][i].v[c]), acc[i][c]);
+                for (int c = 0; c < UNIT<T>; ++c) acc[c] = fmaf(w[q], to_float(u[q].v[c]), acc[c]);
             }
     }
+    Unit<T> o;
 #pragma unroll
-    for (int i = 0; i < UN; ++i) {
-        const int64_t k = k0 + i * L * UNIT<T>;
-        Unit<T> u;
-#pragma unroll
-        for (int c = 0; c < UNIT<T>; ++c) u.v[c] = (T)acc[i][c];
-        if (k < H) store_unit(out + n * out_stride + k, H - k, u);
-    }
+    for (int c = 0; c < UNIT<T>; ++c) o.v[c] = (T)acc[c];
+    store_unit(out + n * out_stride + k, H - k, o);
 }
 
 // The rows of a sample are gone through by L lanes (256: the whole workgroup), S slots at a time: the gradient of the
@@ -734,20 +712,16 @@ __global__ __launch_bounds__(256) void k_combine_backward(const T* __restrict__ 
     }
 }
 
-// f(integral_constant<L>, integral_constant<UN>) for rows of `units` units
+// f(integral_constant<L>) for rows of `units` units
 template <class F>
 void row_lanes(int64_t units, F&& f) {
-#define EINET_L(LL, UU) f(std::integral_constant<int, LL>{}, std::integral_constant<int, UU>{})
-    if (units <= 1) EINET_L(1, 1);
-    else if (units <= 2) EINET_L(2, 1);
-    else if (units <= 4) EINET_L(4, 1);
-    else if (units <= 8) EINET_L(8, 1);
-    else if (units <= 16) EINET_L(16, 1);
-    else if (units <= 32) EINET_L(32, 1);
-    else if (units <= 64) EINET_L(64, 1);
-    else if (units <= 128) EINET_L(64, 2);
-    else EINET_L(64, 4);
-#undef EINET_L
+    if (units <= 1) f(std::integral_constant<int, 1>{});
+    else if (units <= 2) f(std::integral_constant<int, 2>{});
+    else if (units <= 4) f(std::integral_constant<int, 4>{});
+    else if (units <= 8) f(std::integral_constant<int, 8>{});
+    else if (units <= 16) f(std::integral_constant<int, 16>{});
+    else if (units <= 32) f(std::integral_constant<int, 32>{});
+    else f(std::integral_constant<int, 64>{});
 }
 
 }  // namespace
@@ -783,13 +757,16 @@ void launch_route(const Scores& a, int top, bool renormalise, int32_t* ids, floa
     });
 }
 
-size_t route_backward_workspace(int M, int64_t N) { return sizeof(float) * (size_t)route_backward_groups(N) * M; }
+size_t route_backward_workspace(int M, int64_t N) {
+    const int groups = route_backward_groups(M, N);
+    return groups > 1 ? sizeof(float) * (size_t)groups * M : 0;
+}
 
 void launch_route_backward(const Scores& a, int top, bool renormalise, const int32_t* ids, const float* weights,
                            const float* dweights, const float* dlogp, void* dscores, int64_t dsc, int64_t dsn, float* dcoef,
                            void* workspace, hipStream_t s) {
-    const int groups = route_backward_groups(a.N), re = renormalise ? 1 : 0;
-    float* const partial = dcoef ? static_cast<float*>(workspace) : nullptr;
+    const int groups = route_backward_groups(a.M, a.N), re = renormalise ? 1 : 0;
+    float* const partial = !dcoef ? nullptr : groups > 1 ? static_cast<float*>(workspace) : dcoef;
     if (a.N > 0)
         route_types(a, [&](auto t, auto k) {
             using T = decltype(t);
@@ -807,7 +784,8 @@ void launch_route_backward(const Scores& a, int top, bool renormalise, const int
                                    top, re, ids, weights, dweights, dlogp, d, dsc, dsn, partial);
             });
         });
-    if (dcoef) hipLaunchKernelGGL(k_route_coef, dim3((a.M + 31) / 32), dim3(1024), 0, s, partial, groups, a.M, dcoef);
+    if (dcoef && (groups > 1 || a.N == 0))
+        hipLaunchKernelGGL(k_route_coef, dim3((a.M + 31) / 32), dim3(1024), 0, s, partial, a.N > 0 ? groups : 0, a.M, dcoef);
 }
 
 size_t sort_workspace(int64_t slots, int M) {
@@ -826,11 +804,11 @@ void launch_sort(const int32_t* ids, int64_t slots, int M, int32_t* first, int32
     hipLaunchKernelGGL(k_sort, dim3(blocks), dim3(64 * SORT_WAVES), lds, s, ids, slots, M, bits, counts, first, place);
 }
 
-// Rows are split into launches of fewer than 2^32 items, and of fewer than 2^31 workgroups: f(first sample, samples).
+// Samples in launches of fewer than 2^31 items: f(first sample, samples).
 template <class F>
 void row_batches(int64_t N, int64_t tiles, F&& f) {
-    const int64_t most = (int64_t)0x7fffffff / tiles > 0 ? (int64_t)0x7fffffff / tiles : 1;
-    for (int64_t n0 = 0; n0 < N; n0 += most) f(n0, N - n0 < most ? N - n0 : most);
+    const int64_t most = std::max<int64_t>(0x7fffffff / tiles, 1);
+    for (int64_t n0 = 0; n0 < N; n0 += most) f(n0, std::min(N - n0, most));
 }
 
 void launch_dispatch(const void* x, int64_t row_bytes, int64_t x_stride, int64_t N, int top, const int32_t* place, void* out,
@@ -842,11 +820,11 @@ void launch_dispatch(const void* x, int64_t row_bytes, int64_t x_stride, int64_t
         using T = decltype(t);
         constexpr int64_t e = sizeof(T);
         const int64_t H = row_bytes / e, units = (H + UNIT<T> - 1) / UNIT<T>;
-        row_lanes(units, [&](auto l, auto un) {
-            constexpr int L = decltype(l)::value, UN = decltype(un)::value;
-            const int64_t tiles = (units + L * UN - 1) / (L * UN);
+        row_lanes(units, [&](auto l) {
+            constexpr int L = decltype(l)::value;
+            const int64_t tiles = (units + L - 1) / L;
             row_batches(N, tiles, [&](int64_t n0, int64_t n) {
-                hipLaunchKernelGGL((k_dispatch<T, L, UN>), dim3((unsigned)((n * tiles + 256 / L - 1) / (256 / L))), dim3(256), 0, s,
+                hipLaunchKernelGGL((k_dispatch<T, L>), dim3((unsigned)((n * tiles + 256 / L - 1) / (256 / L))), dim3(256), 0, s,
                                    static_cast<const T*>(x) + n0 * (x_stride / e), H, x_stride / e, n, (int)tiles, top,
                                    place + n0 * top, static_cast<T*>(out), out_stride / e, out_rows);
             });
@@ -857,25 +835,30 @@ void launch_dispatch(const void* x, int64_t row_bytes, int64_t x_stride, int64_t
     else go(uint8_t{});
 }
 
+// f(integral_constant<S>) for the slots whose rows are in flight together
+template <class F>
+void slots_together(int top, F&& f) {
+    if (top == 1) f(std::integral_constant<int, 1>{});
+    else if (top == 2) f(std::integral_constant<int, 2>{});
+    else f(std::integral_constant<int, 4>{});
+}
+
 void launch_combine(const void* rows, int type, int64_t H, int64_t stride, int64_t n_rows, const int32_t* place,
                     const float* weights, int64_t N, int top, void* out, int64_t out_stride, hipStream_t s) {
     if (N == 0 || H == 0) return;
     with_type(type, [&](auto t) {
         using T = decltype(t);
         const int64_t units = (H + UNIT<T> - 1) / UNIT<T>;
-        row_lanes(units, [&](auto l, auto un) {
-            constexpr int L = decltype(l)::value, UN = decltype(un)::value;
-            const int64_t tiles = (units + L * UN - 1) / (L * UN);
+        row_lanes(units, [&](auto l) {
+            constexpr int L = decltype(l)::value;
+            const int64_t tiles = (units + L - 1) / L;
             row_batches(N, tiles, [&](int64_t n0, int64_t n) {
-                const dim3 grid((unsigned)((n * tiles + 256 / L - 1) / (256 / L)));
-                const T* const r = static_cast<const T*>(rows);
-                T* const o = static_cast<T*>(out) + n0 * out_stride;
-                const int32_t* const at = place + n0 * top;
-                const float* const w = weights ? weights + n0 * top : nullptr;
-                if (top == 1)
-                    hipLaunchKernelGGL((k_combine<T, L, UN, 1>), grid, dim3(256), 0, s, r, H, stride, n_rows, at, w, n, (int)tiles, top, o, out_stride);
-                else
-                    hipLaunchKernelGGL((k_combine<T, L, UN, 2>), grid, dim3(256), 0, s, r, H, stride, n_rows, at, w, n, (int)tiles, top, o, out_stride);
+                slots_together(top, [&](auto q) {
+                    hipLaunchKernelGGL((k_combine<T, L, decltype(q)::value>), dim3((unsigned)((n * tiles + 256 / L - 1) / (256 / L))),
+                                       dim3(256), 0, s, static_cast<const T*>(rows), H, stride, n_rows, place + n0 * top,
+                                       weights ? weights + n0 * top : nullptr, n, (int)tiles, top,
+                                       static_cast<T*>(out) + n0 * out_stride, out_stride);
+                });
             });
         });
     });
@@ -890,20 +873,14 @@ void launch_combine_backward(const void* dout, int64_t dout_stride, const void* 
         const int64_t units = (H + UNIT<T> - 1) / UNIT<T>;
         auto go = [&](auto l) {
             constexpr int L = decltype(l)::value;
-            const dim3 grid((unsigned)((N + 256 / L - 1) / (256 / L)));
-            const T* const g = static_cast<const T*>(dout);
-            const T* const r = static_cast<const T*>(rows);
-            T* const d = static_cast<T*>(drows);
-            if (top == 1)
-                hipLaunchKernelGGL((k_combine_backward<T, L, 1>), grid, dim3(256), 0, s, g, dout_stride, r, H, stride, n_rows, place, weights, N, top, d, drows_stride, dweights);
-            else if (top == 2)
-                hipLaunchKernelGGL((k_combine_backward<T, L, 2>), grid, dim3(256), 0, s, g, dout_stride, r, H, stride, n_rows, place, weights, N, top, d, drows_stride, dweights);
-            else
-                hipLaunchKernelGGL((k_combine_backward<T, L, 4>), grid, dim3(256), 0, s, g, dout_stride, r, H, stride, n_rows, place, weights, N, top, d, drows_stride, dweights);
+            slots_together(top, [&](auto q) {
+                hipLaunchKernelGGL((k_combine_backward<T, L, decltype(q)::value>), dim3((unsigned)((N + 256 / L - 1) / (256 / L))),
+                                   dim3(256), 0, s, static_cast<const T*>(dout), dout_stride, static_cast<const T*>(rows), H, stride,
+                                   n_rows, place, weights, N, top, static_cast<T*>(drows), drows_stride, dweights);
+            });
         };
-        // (few samples with long rows: a workgroup each instead of a wave)
-        if (units > 64 && N < 8 * EINET_NUM_CUS) go(std::integral_constant<int, 256>{});
-        else row_lanes(units, [&](auto l, auto) { go(l); });
+        if (units > 64) go(std::integral_constant<int, 256>{});
+        else row_lanes(units, go);
     });
 }
 

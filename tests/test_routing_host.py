@@ -43,11 +43,11 @@ def test_route_refusals():
 def test_route_backward_refusals():
     lib = P.load_library()
     size = C.c_size_t()
-    assert lib.einet_route_workspace(4, 8, C.byref(size)) == 0 and size.value > 0
+    assert lib.einet_route_workspace(4, 800, C.byref(size)) == 0 and size.value > 0
     _refused(lib.einet_route_workspace(0, 8, C.byref(size)), "n_components")
     _refused(lib.einet_route_workspace(4, 8, None), "bytes")
 
-    def call(score=X, M=4, n=8, top=2, ids=X, w=X, dw=X, dl=X, ds=X, dsc=8, dsn=1, da=X, ws=X, size=size.value):
+    def call(score=X, M=4, n=800, top=2, ids=X, w=X, dw=X, dl=X, ds=X, dsc=8, dsn=1, da=X, ws=X, size=size.value):
         return lib.einet_route_backward(score, 0, 8, 1, None, M, n, top, 0, ids, w, dw, dl, ds, dsc, dsn, da, ws, size, None)
 
     _refused(call(M=0), "n_components")
