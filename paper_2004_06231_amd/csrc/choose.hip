@@ -308,11 +308,15 @@ __global__ __launch_bounds__(256) void k_choose_wave(ChooseArgs a, int shift) {
                 if (near > lo && near < hi) mid = near;
             }
             uint32_t part = 0;
+            int n = 0;
 #pragma unroll
-            for (int e = 0; e < E; ++e) part += k[e] >= mid ? upper[e] : 0u;
+            for (int e = 0; e < E; ++e) {
+                const bool in = k[e] >= mid;
+                part += in ? upper[e] : 0u;
+                n += __popcll(__ballot(in));
+            }
             const u64 sum = wave_reduce(part, OpAdd{});
             const bool enough = (sum << 31) >= mass || (((sum + V) << 31) > mass && mass_from(mid) >= mass);
-            const int n = count_from(mid);
             if (enough) lo = mid, n_lo = n, guess = 0.5f;
             else hi = mid, n_hi = n, guess = 8.f;
         }

@@ -149,54 +149,64 @@ __global__ __launch_bounds__(256) void k_route(const T* __restrict__ p, int64_t 
 }
 
 // A sample to a lane, for components whose samples are next to each other: the loads of a component are contiguous over
-// the lanes.  The scores are gone through twice, for the maximum with the selections and for the sum.
+// the lanes.  Up to KEPT components stay in registers; of more, the scores are read again for the sum.
 constexpr int ROUTE_COLUMNS_MOST = 128;              // components: the eight running sums of z add up 16 terms at most
-template <class T, class K, int TOP>
+template <class T, class K, int TOP, int KEPT>
 __global__ __launch_bounds__(256) void k_route_columns(const T* __restrict__ p, int64_t sc, const float* __restrict__ coef, int M,
                                                        int64_t N, int top, int renormalise, int32_t* __restrict__ ids,
                                                        float* __restrict__ weights, float* __restrict__ logp) {
     const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (n >= N) return;
     p += n;
+    T x[KEPT > 0 ? KEPT : 8];
+    if constexpr (KEPT > 0) {
+#pragma unroll
+        for (int c = 0; c < KEPT; ++c) x[c] = p[min(c, M - 1) * sc];
+    }
+    // f(component, score) for all components, eight at a time
+    auto each = [&](auto f) {
+        if constexpr (KEPT > 0) {
+#pragma unroll
+            for (int c0 = 0; c0 < KEPT; c0 += 8) {
+                if (c0 >= M) break;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (c0 + i < M) f(c0 + i, i, x[c0 + i]);
+            }
+        } else {
+            for (int c0 = 0; c0 < M; c0 += 8) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = p[min(c0 + i, M - 1) * sc];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (c0 + i < M) f(c0 + i, i, x[i]);
+            }
+        }
+    };
     K best[TOP];
     int id[TOP];
 #pragma unroll
     for (int s = 0; s < TOP; ++s) best[s] = (K)-INFINITY, id[s] = -1;
-    for (int c0 = 0; c0 < M; c0 += 8) {
-        T x[8];
+    each([&](int c, int, T score) {
+        const K t = route_sum<K>(score, coef, c);
+        if (!(t > best[TOP - 1])) return;                    // (equal ones stay behind the lower component)
+        best[TOP - 1] = t;
+        id[TOP - 1] = c;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = p[min(c0 + i, M - 1) * sc];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int c = c0 + i;
-            K t = c < M ? route_sum<K>(x[i], coef, min(c, M - 1)) : (K)-INFINITY;
-            if (!(t > best[TOP - 1])) continue;              // (equal ones stay behind the lower component)
-            best[TOP - 1] = t;
-            id[TOP - 1] = c;
-#pragma unroll
-            for (int s = TOP - 1; s > 0; --s)
-                if (best[s] > best[s - 1]) {
-                    const K b = best[s];
-                    const int k = id[s];
-                    best[s] = best[s - 1], id[s] = id[s - 1];
-                    best[s - 1] = b, id[s - 1] = k;
-                }
-        }
-    }
+        for (int s = TOP - 1; s > 0; --s)
+            if (best[s] > best[s - 1]) {
+                const K b = best[s];
+                const int k = id[s];
+                best[s] = best[s - 1], id[s] = id[s - 1];
+                best[s - 1] = b, id[s - 1] = k;
+            }
+    });
     const K m = best[0];
     const bool dead = !(m > (K)-INFINITY);
     float sums[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sums[i] = 0.f;
-    if (!dead)
-        for (int c0 = 0; c0 < M; c0 += 8) {
-            T x[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = p[min(c0 + i, M - 1) * sc];
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c0 + i < M) sums[i] += route_exp(route_sum<K>(x[i], coef, c0 + i), m);
-        }
+    if (!dead) each([&](int c, int i, T score) { sums[i] += route_exp(route_sum<K>(score, coef, c), m); });
     const float z = ((sums[0] + sums[1]) + (sums[2] + sums[3])) + ((sums[4] + sums[5]) + (sums[6] + sums[7]));
     float e[TOP], total = 0.f;
 #pragma unroll
@@ -744,9 +754,18 @@ void launch_route(const Scores& a, int top, bool renormalise, int32_t* ids, floa
         const T* const p = static_cast<const T*>(a.p);
         if (route_by_columns(a, top)) {
             const dim3 grid((unsigned)((a.N + 255) / 256));
-            if (top == 1) hipLaunchKernelGGL((k_route_columns<T, K, 1>), grid, dim3(256), 0, s, p, a.sc, a.coef, a.M, a.N, top, re, ids, weights, logp);
-            else if (top == 2) hipLaunchKernelGGL((k_route_columns<T, K, 2>), grid, dim3(256), 0, s, p, a.sc, a.coef, a.M, a.N, top, re, ids, weights, logp);
-            else hipLaunchKernelGGL((k_route_columns<T, K, 4>), grid, dim3(256), 0, s, p, a.sc, a.coef, a.M, a.N, top, re, ids, weights, logp);
+            auto go = [&](auto most, auto kept) {
+                hipLaunchKernelGGL((k_route_columns<T, K, decltype(most)::value, decltype(kept)::value>), grid, dim3(256), 0, s, p, a.sc,
+                                   a.coef, a.M, a.N, top, re, ids, weights, logp);
+            };
+            auto with_top = [&](auto kept) {
+                if (top == 1) go(std::integral_constant<int, 1>{}, kept);
+                else if (top == 2) go(std::integral_constant<int, 2>{}, kept);
+                else go(std::integral_constant<int, 4>{}, kept);
+            };
+            if (a.M <= 16) with_top(std::integral_constant<int, 16>{});
+            else if (a.M <= 64) with_top(std::integral_constant<int, 64>{});
+            else with_top(std::integral_constant<int, 0>{});
             return;
         }
         route_variant(a.M, top, [&](auto g, auto e) {
