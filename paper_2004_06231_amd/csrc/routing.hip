@@ -105,15 +105,47 @@ __device__ __forceinline__ K route_load(const T* __restrict__ p, int64_t sc, int
     return group_reduce<G>(m, Larger{});
 }
 
+// Where the samples of a component are next to each other, the scores of ROUTE_STAGE samples come through LDS: read along the
+// samples, handed out along the components.  Rows of M | 1 floats: neither way meets a bank twice.
+template <int G> constexpr int ROUTE_STAGE = G == 64 ? 8 : 32;
+template <int G, bool STAGED> constexpr int ROUTE_THREADS = STAGED ? ROUTE_STAGE<G> * G : 256;
+
+template <class T, int G>
+__device__ __forceinline__ void stage_scores(const T* __restrict__ p, int64_t sc, int M, int64_t n0, int64_t N, float* tile) {
+    constexpr int S = ROUTE_STAGE<G>;
+    const int s = threadIdx.x % S, wide = M | 1;
+    const bool there = n0 + s < N;
+#pragma unroll 4
+    for (int c = threadIdx.x / S; c < M; c += G) tile[s * wide + c] = there ? to_float(p[c * sc + n0 + s]) : -INFINITY;
+    __syncthreads();
+}
 template <class T, class K, int G, int E>
-__global__ __launch_bounds__(256) void k_route(const T* __restrict__ p, int64_t sc, int64_t sn, const float* __restrict__ coef,
+__device__ __forceinline__ K staged_load(const float* tile, const float* __restrict__ coef, int M, int j, K (&t)[E]) {
+    const float* const row = tile + threadIdx.x / G * (M | 1);
+    K m = (K)-INFINITY;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int c = route_component<T, G, E>(e, j);
+        t[e] = c < M ? route_sum<K>(row[c], coef, c) : (K)-INFINITY;
+        m = Larger{}(m, t[e]);
+    }
+    return group_reduce<G>(m, Larger{});
+}
+
+template <class T, class K, int G, int E, bool STAGED>
+__global__ __launch_bounds__((ROUTE_THREADS<G, STAGED>)) void k_route(const T* __restrict__ p, int64_t sc, int64_t sn, const float* __restrict__ coef,
                                                int M, int64_t N, int top, int renormalise, int32_t* __restrict__ ids,
                                                float* __restrict__ weights, float* __restrict__ logp) {
+    constexpr int S = ROUTE_THREADS<G, STAGED> / G;
     const int j = threadIdx.x % G;
-    const int64_t n = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
+    const int64_t n = (int64_t)blockIdx.x * S + threadIdx.x / G;
+    extern __shared__ float tile[];
+    if constexpr (STAGED) stage_scores<T, G>(p, sc, M, (int64_t)blockIdx.x * S, N, tile);
     if (n >= N) return;
     K t[E];
-    const K m = route_load<T, K, G, E>(p, sc, sn, coef, M, n, j, t);
+    K m;
+    if constexpr (STAGED) m = staged_load<T, K, G, E>(tile, coef, M, j, t);
+    else m = route_load<T, K, G, E>(p, sc, sn, coef, M, n, j, t);
     const bool dead = !(m > (K)-INFINITY);
     float z = 0.f;
 #pragma unroll
@@ -149,38 +181,25 @@ __global__ __launch_bounds__(256) void k_route(const T* __restrict__ p, int64_t 
 }
 
 // A sample to a lane, for components whose samples are next to each other: the loads of a component are contiguous over
-// the lanes.  Up to KEPT components stay in registers; of more, the scores are read again for the sum.
-constexpr int ROUTE_COLUMNS_MOST = 128;              // components: the eight running sums of z add up 16 terms at most
-template <class T, class K, int TOP, int KEPT>
+// the lanes, and up to MOST components of a sample are in registers.
+constexpr int ROUTE_COLUMNS_MOST = 64;
+template <class T, class K, int TOP, int MOST>
 __global__ __launch_bounds__(256) void k_route_columns(const T* __restrict__ p, int64_t sc, const float* __restrict__ coef, int M,
                                                        int64_t N, int top, int renormalise, int32_t* __restrict__ ids,
                                                        float* __restrict__ weights, float* __restrict__ logp) {
     const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (n >= N) return;
-    p += n;
-    T x[KEPT > 0 ? KEPT : 8];
-    if constexpr (KEPT > 0) {
+    T x[MOST];
 #pragma unroll
-        for (int c = 0; c < KEPT; ++c) x[c] = p[min(c, M - 1) * sc];
-    }
-    // f(component, score) for all components, eight at a time
+    for (int c = 0; c < MOST; ++c) x[c] = p[n + min(c, M - 1) * sc];
+    // f(component, one of eight, score) for all components
     auto each = [&](auto f) {
-        if constexpr (KEPT > 0) {
 #pragma unroll
-            for (int c0 = 0; c0 < KEPT; c0 += 8) {
-                if (c0 >= M) break;
+        for (int c0 = 0; c0 < MOST; c0 += 8) {
+            if (c0 >= M) break;
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (c0 + i < M) f(c0 + i, i, x[c0 + i]);
-            }
-        } else {
-            for (int c0 = 0; c0 < M; c0 += 8) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = p[min(c0 + i, M - 1) * sc];
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (c0 + i < M) f(c0 + i, i, x[i]);
-            }
+            for (int i = 0; i < 8; ++i)
+                if (c0 + i < M) f(c0 + i, i, x[c0 + i]);
         }
     };
     K best[TOP];
@@ -230,24 +249,29 @@ __global__ __launch_bounds__(256) void k_route_columns(const T* __restrict__ p, 
 // The log-density and the weights are differences and quotients of numbers rounded to float32; m and z come from the
 // scores again.  d coef[c] = sum_n d t[c][n]: a lane has the same components for all its samples and adds their gradients
 // up in registers; the workgroup's sums go to a row of the workspace, which the second kernel adds up in a fixed order.
-template <class T, class K, int G, int E>
-__global__ __launch_bounds__(256) void k_route_backward(const T* __restrict__ p, int64_t sc, int64_t sn,
+template <class T, class K, int G, int E, bool STAGED>
+__global__ __launch_bounds__((ROUTE_THREADS<G, STAGED>)) void k_route_backward(const T* __restrict__ p, int64_t sc, int64_t sn,
                                                         const float* __restrict__ coef, int M, int64_t N, int top,
                                                         int renormalise, const int32_t* __restrict__ ids,
                                                         const float* __restrict__ weights, const float* __restrict__ dweights,
                                                         const float* __restrict__ dlogp, T* __restrict__ dscores, int64_t dsc,
                                                         int64_t dsn, float* __restrict__ partial) {
-    constexpr int S = 256 / G, VEC = ROUTE_VEC<T, E>;
+    constexpr int NT = ROUTE_THREADS<G, STAGED>, S = NT / G, VEC = ROUTE_VEC<T, E>;
     struct Pack { T v[VEC]; };
+    extern __shared__ float tile[];
     const int j = threadIdx.x % G;
     float acc[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = 0.f;
     for (int64_t n0 = (int64_t)blockIdx.x * S; n0 < N; n0 += (int64_t)gridDim.x * S) {
-        const int64_t n = n0 + threadIdx.x / G;
-        if (n >= N) continue;                                   // (whole groups leave together)
+        if constexpr (STAGED) stage_scores<T, G>(p, sc, M, n0, N, tile);
+        // (the samples behind the last one are the last one again, and count for nothing)
+        const bool there = n0 + threadIdx.x / G < N;
+        const int64_t n = there ? n0 + threadIdx.x / G : N - 1;
         K t[E];
-        const K m = route_load<T, K, G, E>(p, sc, sn, coef, M, n, j, t);
+        K m;
+        if constexpr (STAGED) m = staged_load<T, K, G, E>(tile, coef, M, j, t);
+        else m = route_load<T, K, G, E>(p, sc, sn, coef, M, n, j, t);
         const bool dead = !(m > (K)-INFINITY);
         float z = 0.f;
         float d[E];
@@ -277,6 +301,22 @@ __global__ __launch_bounds__(256) void k_route_backward(const T* __restrict__ p,
                 for (int e = 0; e < E; ++e)
                     if (c == route_component<T, G, E>(e, j)) d[e] += v;
             }
+        if constexpr (STAGED) {
+            float* const mine = tile + threadIdx.x / G * (M | 1);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int c = route_component<T, G, E>(e, j);
+                if (c < M) mine[c] = d[e];
+                if (there) acc[e] += d[e];
+            }
+            __syncthreads();
+            const int s = threadIdx.x % S;
+            if (n0 + s < N)
+                for (int c = threadIdx.x / S; c < M; c += G) dscores[c * dsc + n0 + s] = (T)tile[s * (M | 1) + c];
+            __syncthreads();
+            continue;
+        }
+        if (!there) continue;
         T* const row = dscores + n * dsn;
 #pragma unroll
         for (int v = 0; v < E / VEC; ++v) {
@@ -296,7 +336,8 @@ __global__ __launch_bounds__(256) void k_route_backward(const T* __restrict__ p,
         for (int e = 0; e < E; ++e) acc[e] += d[e];
     }
     if (!partial) return;
-    __shared__ float sums[4][G * E];
+    constexpr int WAVES = (NT + 63) / 64;
+    __shared__ float sums[WAVES][G * E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         float v = acc[e];
@@ -305,88 +346,109 @@ __global__ __launch_bounds__(256) void k_route_backward(const T* __restrict__ p,
         if ((threadIdx.x & 63) < G) sums[threadIdx.x >> 6][route_component<T, G, E>(e, j)] = v;
     }
     __syncthreads();
-    for (int c = threadIdx.x; c < M; c += 256)
-        partial[(size_t)blockIdx.x * M + c] = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
+    for (int c = threadIdx.x; c < M; c += NT) {
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) v += sums[w][c];
+        partial[(size_t)blockIdx.x * M + c] = v;
+    }
 }
 
-// The same with a sample to a lane.  The gradients of a component are added up over the lanes of a wave as they arise.
-template <class T, class K>
+// The same with a sample to a lane and up to MOST components in registers.  The gradients of a component are summed over the
+// lanes by folding: a step adds two halves of the lanes and keeps of every pair of components one in each half, so that 64
+// components take 63 additions, not 64 times 6, and lane l is left with the sum of component l (16: with that of l % 16).
+template <int CTRL>
+__device__ __forceinline__ float fold(float a, float b, bool second) {
+    return (second ? b : a) + lane_of<CTRL>(second ? a : b);
+}
+template <int MOST>
+__device__ __forceinline__ float fold_lanes(float (&d)[MOST]) {
+    const int lane = threadIdx.x & 63;
+    if constexpr (MOST == 64) {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+            const auto v = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, d[c]), __builtin_bit_cast(uint32_t, d[c + 32]), false, false);
+            const uint32_t v0 = v[0], v1 = v[1];
+            d[c] = __builtin_bit_cast(float, v0) + __builtin_bit_cast(float, v1);
+        }
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+            const auto v = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, d[c]), __builtin_bit_cast(uint32_t, d[c + 16]), false, false);
+            const uint32_t v0 = v[0], v1 = v[1];
+            d[c] = __builtin_bit_cast(float, v0) + __builtin_bit_cast(float, v1);
+        }
+    }
+    // (partners: rotated by eight, mirrored in eight, mirrored in four, neighbours)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) d[c] = fold<0x128>(d[c], d[c + 8], lane & 8);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) d[c] = fold<0x141>(d[c], d[c + 4], lane & 4);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) d[c] = fold<0x1B>(d[c], d[c + 2], lane & 2);
+    float r = fold<0xB1>(d[0], d[1], lane & 1);
+    if constexpr (MOST == 16) {
+        r += __shfl_xor(r, 16, 64);
+        r += __shfl_xor(r, 32, 64);
+    }
+    return r;
+}
+
+template <class T, class K, int TOP, int MOST>
 __global__ __launch_bounds__(256) void k_route_backward_columns(const T* __restrict__ p, int64_t sc, const float* __restrict__ coef,
                                                                 int M, int64_t N, int top, int renormalise,
                                                                 const int32_t* __restrict__ ids, const float* __restrict__ weights,
                                                                 const float* __restrict__ dweights, const float* __restrict__ dlogp,
                                                                 T* __restrict__ dscores, int64_t dsc, float* __restrict__ partial) {
-    __shared__ float sums[4][ROUTE_COLUMNS_MOST];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int c = lane; c < M; c += 64) sums[wave][c] = 0.f;     // (a wave's own, by lane 63 only from here on)
-    __syncthreads();
+    float acc = 0.f;                                            // of component lane % MOST, over the wave's samples
     for (int64_t n0 = (int64_t)blockIdx.x * 256; n0 < N; n0 += (int64_t)gridDim.x * 256) {
         const bool there = n0 + threadIdx.x < N;
         const int64_t n = there ? n0 + threadIdx.x : N - 1;
-        const T* const x = p + n;
+        float d[MOST];
+#pragma unroll
+        for (int c = 0; c < MOST; ++c) d[c] = to_float(p[n + min(c, M - 1) * sc]);
         K m = (K)-INFINITY;
-        for (int c0 = 0; c0 < M; c0 += 8) {
-            T v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = x[min(c0 + i, M - 1) * sc];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) m = Larger{}(m, route_sum<K>(v[i], coef, min(c0 + i, M - 1)));
-        }
+        for (int c = 0; c < MOST; ++c)
+            if (c < M) m = Larger{}(m, route_sum<K>(d[c], coef, c));
         const bool dead = !(m > (K)-INFINITY);
         float part[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) part[i] = 0.f;
-        for (int c0 = 0; c0 < M; c0 += 8) {
-            T v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = x[min(c0 + i, M - 1) * sc];
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c0 + i < M) part[i] += dead ? 0.f : route_exp(route_sum<K>(v[i], coef, c0 + i), m);
+        for (int c = 0; c < MOST; ++c) {
+            d[c] = c < M ? route_exp(route_sum<K>(d[c], coef, c), m) : 0.f;
+            part[c % 8] += d[c];
         }
         const float z = ((part[0] + part[1]) + (part[2] + part[3])) + ((part[4] + part[5]) + (part[6] + part[7]));
-        int id[4];
-        float add[4], a = 0.f;
+        int id[TOP];
+        float add[TOP], a = 0.f;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
+        for (int s = 0; s < TOP; ++s) {
             id[s] = s < top && dweights ? ids[n * top + s] : -1;
             add[s] = id[s] >= 0 ? weights[n * top + s] * dweights[n * top + s] : 0.f;
             a += add[s];
         }
         if (renormalise) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
+            for (int s = 0; s < TOP; ++s)
                 if (id[s] >= 0) add[s] = weights[n * top + s] * (dweights[n * top + s] - a);
         }
         const float dl = dlogp ? dlogp[n] : 0.f;
-        const float scale = dead ? 0.f : (renormalise ? dl : dl - a) / z;
-        for (int c0 = 0; c0 < M; c0 += 8) {
-            T v[8];
+        const float scale = (renormalise ? dl : dl - a) / z;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = x[min(c0 + i, M - 1) * sc];
+        for (int c = 0; c < MOST; ++c) {
+            float v = d[c] * scale;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int c = c0 + i;
-                if (c >= M) break;
-                float d = dead ? 0.f : route_exp(route_sum<K>(v[i], coef, c), m) * scale;
-#pragma unroll
-                for (int s = 0; s < 4; ++s)
-                    if (id[s] == c) d += add[s];
-                if (there) dscores[c * dsc + n] = (T)d;
-                if (partial) {
-                    float r = there ? d : 0.f;
-                    r += lane_of<0xB1>(r);
-                    r += lane_of<0x4E>(r);
-                    r += lane_of<0x141>(r);
-                    r += lane_of<0x140>(r);
-                    r += __shfl_xor(r, 16, 64);
-                    r += __shfl_xor(r, 32, 64);
-                    if (lane == 63) sums[wave][c] += r;
-                }
-            }
+            for (int s = 0; s < TOP; ++s) v += id[s] == c ? add[s] : 0.f;
+            d[c] = dead || !there ? 0.f : v;
+            if (there && c < M) dscores[n + c * dsc] = (T)d[c];
         }
+        if (partial) acc += fold_lanes<MOST>(d);
     }
     if (!partial) return;
+    __shared__ float sums[4][MOST];
+    if (lane < MOST) sums[wave][lane] = acc;
     __syncthreads();
     for (int c = threadIdx.x; c < M; c += 256)
         partial[(size_t)blockIdx.x * M + c] = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
@@ -421,6 +483,9 @@ int route_lanes(int M, int top) {
 // A sample to a lane: where the samples of a component are next to each other and there are enough of them for every
 // compute unit to have two workgroups' worth of lanes.
 bool route_by_columns(const Scores& a, int top) { return a.sn == 1 && a.M <= ROUTE_COLUMNS_MOST && top <= 4 && a.N >= 2 * 256 * EINET_NUM_CUS; }
+// Through LDS: such scores of fewer samples, more components or more selections.
+bool route_staged(const Scores& a) { return a.sn == 1 && a.sc != 1 && a.N >= 16 * EINET_NUM_CUS; }
+template <int G> size_t route_tile_bytes(int M) { return sizeof(float) * ROUTE_STAGE<G> * (size_t)(M | 1); }
 
 // Workgroups of the gradient, which is the rows of its workspace.  A handful of samples are one workgroup's, whose sums are
 // the gradient of the coefficients: no second launch and no workspace.
@@ -736,6 +801,18 @@ void row_lanes(int64_t units, F&& f) {
 
 }  // namespace
 
+// f(integral_constant<TOP>, integral_constant<MOST>) for the selections and components of a lane's sample
+template <class F>
+void columns_variant(int M, int top, F&& f) {
+    auto with = [&](auto most) {
+        if (top == 1) f(std::integral_constant<int, 1>{}, most);
+        else if (top == 2) f(std::integral_constant<int, 2>{}, most);
+        else f(std::integral_constant<int, 4>{}, most);
+    };
+    if (M <= 16) with(std::integral_constant<int, 16>{});
+    else with(std::integral_constant<int, ROUTE_COLUMNS_MOST>{});
+}
+
 // f(T{}, K{}) for the types of the scores and of their sums with the coefficients
 template <class F>
 void route_types(const Scores& a, F&& f) {
@@ -754,24 +831,22 @@ void launch_route(const Scores& a, int top, bool renormalise, int32_t* ids, floa
         const T* const p = static_cast<const T*>(a.p);
         if (route_by_columns(a, top)) {
             const dim3 grid((unsigned)((a.N + 255) / 256));
-            auto go = [&](auto most, auto kept) {
-                hipLaunchKernelGGL((k_route_columns<T, K, decltype(most)::value, decltype(kept)::value>), grid, dim3(256), 0, s, p, a.sc,
-                                   a.coef, a.M, a.N, top, re, ids, weights, logp);
-            };
-            auto with_top = [&](auto kept) {
-                if (top == 1) go(std::integral_constant<int, 1>{}, kept);
-                else if (top == 2) go(std::integral_constant<int, 2>{}, kept);
-                else go(std::integral_constant<int, 4>{}, kept);
-            };
-            if (a.M <= 16) with_top(std::integral_constant<int, 16>{});
-            else if (a.M <= 64) with_top(std::integral_constant<int, 64>{});
-            else with_top(std::integral_constant<int, 0>{});
+            columns_variant(a.M, top, [&](auto most, auto components) {
+                hipLaunchKernelGGL((k_route_columns<T, K, decltype(most)::value, decltype(components)::value>), grid, dim3(256), 0, s, p,
+                                   a.sc, a.coef, a.M, a.N, top, re, ids, weights, logp);
+            });
             return;
         }
         route_variant(a.M, top, [&](auto g, auto e) {
             constexpr int G = decltype(g)::value, E = decltype(e)::value;
-            hipLaunchKernelGGL((k_route<T, K, G, E>), dim3((unsigned)((a.N + 256 / G - 1) / (256 / G))), dim3(256), 0, s, p, a.sc,
-                               a.sn, a.coef, a.M, a.N, top, re, ids, weights, logp);
+            auto go = [&](auto staged) {
+                constexpr bool STAGED = decltype(staged)::value;
+                constexpr int NT = ROUTE_THREADS<G, STAGED>, S = NT / G;
+                hipLaunchKernelGGL((k_route<T, K, G, E, STAGED>), dim3((unsigned)((a.N + S - 1) / S)), dim3(NT),
+                                   STAGED ? route_tile_bytes<G>(a.M) : 0, s, p, a.sc, a.sn, a.coef, a.M, a.N, top, re, ids, weights, logp);
+            };
+            if (route_staged(a)) go(std::true_type{});
+            else go(std::false_type{});
         });
     });
 }
@@ -793,14 +868,22 @@ void launch_route_backward(const Scores& a, int top, bool renormalise, const int
             const T* const p = static_cast<const T*>(a.p);
             T* const d = static_cast<T*>(dscores);
             if (route_by_columns(a, top) && dsn == 1) {
-                hipLaunchKernelGGL((k_route_backward_columns<T, K>), dim3(groups), dim3(256), 0, s, p, a.sc, a.coef, a.M, a.N, top,
-                                   re, ids, weights, dweights, dlogp, d, dsc, partial);
+                columns_variant(a.M, top, [&](auto most, auto components) {
+                    hipLaunchKernelGGL((k_route_backward_columns<T, K, decltype(most)::value, decltype(components)::value>), dim3(groups),
+                                       dim3(256), 0, s, p, a.sc, a.coef, a.M, a.N, top, re, ids, weights, dweights, dlogp, d, dsc, partial);
+                });
                 return;
             }
             route_variant(a.M, top, [&](auto g, auto e) {
                 constexpr int G = decltype(g)::value, E = decltype(e)::value;
-                hipLaunchKernelGGL((k_route_backward<T, K, G, E>), dim3(groups), dim3(256), 0, s, p, a.sc, a.sn, a.coef, a.M, a.N,
-                                   top, re, ids, weights, dweights, dlogp, d, dsc, dsn, partial);
+                auto go = [&](auto staged) {
+                    constexpr bool STAGED = decltype(staged)::value;
+                    hipLaunchKernelGGL((k_route_backward<T, K, G, E, STAGED>), dim3(groups), dim3(ROUTE_THREADS<G, STAGED>),
+                                       STAGED ? route_tile_bytes<G>(a.M) : 0, s, p, a.sc, a.sn, a.coef, a.M, a.N, top, re, ids, weights,
+                                       dweights, dlogp, d, dsc, dsn, partial);
+                };
+                if (route_staged(a) && dsn == 1) go(std::true_type{});
+                else go(std::false_type{});
             });
         });
     if (dcoef && (groups > 1 || a.N == 0))
