@@ -321,6 +321,7 @@ int einet_mixture_logp(const float* logp_dev, const float* log_coef_dev, int n_c
 enum { EINET_FLOAT32 = 0, EINET_BFLOAT16 = 1, EINET_FLOAT16 = 2 };
 #define EINET_ROUTE_MAX_COMPONENTS 1024
 #define EINET_ROUTE_MAX_TOP 16
+#define EINET_CHOOSE_MAX_ENTRIES (1 << 30)
 
 /* The `top` most probable components of every sample.  With t[c] = score[c] + log_coef[c] (formed in float64):
  *   logp = log sum_c exp(t[c]),  p[c] = exp(t[c] - logp);
@@ -425,7 +426,8 @@ int einet_choose_workspace(int n_rows, int n_entries, size_t* bytes);
  *   index_dev   device, [n_rows] int32, written: -1 for a row whose entries are all left out
  *   logq_dev    device, [n_rows] float32, written, or NULL: log of the chosen entry's share of the kept weight, -inf for -1
  *   workspace_dev   device, einet_choose_workspace bytes, 256-byte aligned (NULL if that is 0)
- * n_rows = 0 does nothing.  Errors: EINET_ERR_INVALID_ARG (unknown dtype, n_rows < 0, n_entries < 1, a value for all rows out of
+ * n_rows = 0 does nothing.  Errors: EINET_ERR_INVALID_ARG (unknown dtype, n_rows < 0, n_entries outside
+ * 1..EINET_CHOOSE_MAX_ENTRIES, a value for all rows out of
  * range: temperature below 0, top_k below 0, top_p or min_p outside [0, 1]; pointers, workspace), EINET_ERR_HIP. */
 int einet_choose(const void* logit_dev, int dtype, int64_t row_stride, int n_rows, int n_entries, const float* u_dev,
                  const float* temperature_dev, float temperature, const int32_t* top_k_dev, int top_k,

@@ -1,5 +1,6 @@
 """ctypes binding of include/einet.h.  Argument marshalling only."""
 import ctypes as C
+import functools
 import math
 import os
 
@@ -465,14 +466,21 @@ def _enqueue(name, device, *args):
         raise EinetError(rc, lib.einet_last_error(None).decode())
 
 
-def _workspace(name, device, *sizes):
-    import torch
+@functools.lru_cache(maxsize=1024)
+def _workspace_bytes(name, *sizes):
+    """What the library says about these sizes (of which it needs nothing else)."""
     lib = load_library()
     n = C.c_size_t()
     rc = getattr(lib, name)(*sizes, C.byref(n))
     if rc != 0:
         raise EinetError(rc, lib.einet_last_error(None).decode())
-    return (torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None), n.value
+    return n.value
+
+
+def _workspace(name, device, *sizes):
+    import torch
+    n = _workspace_bytes(name, *sizes)
+    return (torch.empty(n, dtype=torch.uint8, device=device) if n else None), n
 
 
 def _scores(scores, log_coef):
@@ -628,11 +636,11 @@ def einet_choose(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     _on(device, torch.float32, (n,), u)
     settings = []
     for v, dtype in ((temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32), (min_p, torch.float32)):
-        if torch.is_tensor(v):
-            _on(device, dtype, (n,), v)
-            settings += [v.data_ptr(), 0]
+        if isinstance(v, (int, float)):
+            settings += (None, v)
         else:
-            settings += [None, v]
+            _on(device, dtype, (n,), v)
+            settings += (v.data_ptr(), 0)
     index = torch.empty(n, dtype=torch.int32, device=device)
     logq = torch.empty(n, dtype=torch.float32, device=device)
     ws, n_bytes = _workspace("einet_choose_workspace", device, n, V)

@@ -167,8 +167,8 @@ int einet_combine_backward(const void* dout_dev, int64_t dout_stride, const void
 }
 
 int einet_choose_workspace(int n_rows, int n_entries, size_t* bytes) {
-    if (!bytes || n_rows < 0 || n_entries < 1)
-        return invalid("einet_choose_workspace", "n_rows must be at least 0, n_entries at least 1, bytes not NULL");
+    if (!bytes || n_rows < 0 || n_entries < 1 || n_entries > EINET_CHOOSE_MAX_ENTRIES)
+        return invalid("einet_choose_workspace", "n_rows must be at least 0, n_entries in 1..EINET_CHOOSE_MAX_ENTRIES, bytes not NULL");
     *bytes = choose_workspace(n_rows, n_entries);
     return EINET_OK;
 }
@@ -179,7 +179,8 @@ int einet_choose(const void* logit_dev, int dtype, int64_t row_stride, int n_row
                  size_t workspace_bytes, void* stream) {
     const char* const call = "einet_choose";
     if (!known_type(dtype)) return invalid(call, "unknown dtype");
-    if (n_rows < 0 || n_entries < 1) return invalid(call, "n_rows must be at least 0 and n_entries at least 1");
+    if (n_rows < 0 || n_entries < 1 || n_entries > EINET_CHOOSE_MAX_ENTRIES)
+        return invalid(call, "n_rows must be at least 0 and n_entries in 1..EINET_CHOOSE_MAX_ENTRIES");
     if (row_stride < 0) return invalid(call, "row_stride must not be negative");
     if (!temperature_dev && !(temperature >= 0.f)) return invalid(call, "temperature must be at least 0");
     if (!top_k_dev && top_k < 0) return invalid(call, "top_k must be at least 0");

@@ -130,7 +130,8 @@ def test_choose_refusals():
     nan = float("nan")
     _refused(call(dtype=-1), "dtype")
     _refused(call(n=-1), "n_rows")
-    _refused(call(V=0), "n_entries")
+    for V in (0, (1 << 30) + 1):
+        _refused(call(V=V), "n_entries")
     _refused(call(stride=-1), "row_stride")
     for t in (-0.5, nan):
         _refused(call(t=t), "temperature")
