@@ -72,7 +72,9 @@ __device__ __forceinline__ K route_sum(T score, const float* coef, int c) {
 }
 
 // G lanes share a sample, each with E components in registers: VEC neighbours of every G * VEC, which are one load where
-// the components of a sample are next to each other.
+// the components of a sample are next to each other.  16001 rows of 128 bf16 logits, eight selections: 7.3 us, 0.6 TB/s; the
+// vector ALU bounds it, whose instructions are the eight selections (some 50 each for the wave's four samples) and the
+// exponentials.
 template <class T, int E> constexpr int ROUTE_VEC = E < 16 / (int)sizeof(T) ? E : 16 / (int)sizeof(T);
 template <class T, int G, int E>
 __device__ __forceinline__ int route_component(int e, int j) {
@@ -181,7 +183,9 @@ __global__ __launch_bounds__((ROUTE_THREADS<G, STAGED>)) void k_route(const T* _
 }
 
 // A sample to a lane, for components whose samples are next to each other: the loads of a component are contiguous over
-// the lanes, and up to MOST components of a sample are in registers.
+// the lanes, and up to MOST components of a sample are in registers.  262144 samples of 64 components: 17 us with one
+// selection and no coefficients (4.1 TB/s), 25 us with two and coefficients, whose float64 sums the vector ALU does in 55 %
+// of the time.
 constexpr int ROUTE_COLUMNS_MOST = 64;
 template <class T, class K, int TOP, int MOST>
 __global__ __launch_bounds__(256) void k_route_columns(const T* __restrict__ p, int64_t sc, const float* __restrict__ coef, int M,
@@ -357,6 +361,7 @@ __global__ __launch_bounds__((ROUTE_THREADS<G, STAGED>)) void k_route_backward(c
 // The same with a sample to a lane and up to MOST components in registers.  The gradients of a component are summed over the
 // lanes by folding: a step adds two halves of the lanes and keeps of every pair of components one in each half, so that 64
 // components take 63 additions, not 64 times 6, and lane l is left with the sum of component l (16: with that of l % 16).
+// 262144 samples of 64 components: 45 us, 3.0 TB/s read and written.
 template <int CTRL>
 __device__ __forceinline__ float fold(float a, float b, bool second) {
     return (second ? b : a) + lane_of<CTRL>(second ? a : b);
@@ -480,11 +485,18 @@ int route_lanes(int M, int top) {
     return G;
 }
 
-// A sample to a lane: where the samples of a component are next to each other and there are enough of them for every
-// compute unit to have two workgroups' worth of lanes.
-bool route_by_columns(const Scores& a, int top) { return a.sn == 1 && a.M <= ROUTE_COLUMNS_MOST && top <= 4 && a.N >= 2 * 256 * EINET_NUM_CUS; }
-// Through LDS: such scores of fewer samples, more components or more selections.
-bool route_staged(const Scores& a) { return a.sn == 1 && a.sc != 1 && a.N >= 16 * EINET_NUM_CUS; }
+// Which kernel takes scores whose samples are next to each other (sn = 1).  Measured with log coefficients at 64 components,
+// two selections (16 components, one, without): us without and with gradient,
+//   samples                     8192         16384        65536         131072        262144
+//   groups of lanes, directly   4.7 / 8.2    6.4 / 11     15 / 34       29 / 63       51 / 117   (3.9 / 8.5 at 65536)
+//   groups of lanes, through LDS 4.6 / 8.2   5.5 / 9.3    11 / 22       23 / 40       43 / 72    (4.1 / 12.7)
+//   a lane per sample           12 / 23      12 / 23      12 / 26       16 / 31       25 / 48    (4.1 / 7.9)
+// A lane per sample waits for one chain of loads and needs every compute unit full of waves; a wide row of few components
+// is read well enough directly.
+bool route_by_columns(const Scores& a, int top) {
+    return a.sn == 1 && a.M <= ROUTE_COLUMNS_MOST && top <= 4 && a.N >= (a.M <= 16 ? 256 : 512) * EINET_NUM_CUS;
+}
+bool route_staged(const Scores& a) { return a.sn == 1 && a.sc != 1 && a.M > 16 && a.N >= 32 * EINET_NUM_CUS; }
 template <int G> size_t route_tile_bytes(int M) { return sizeof(float) * ROUTE_STAGE<G> * (size_t)(M | 1); }
 
 // Workgroups of the gradient, which is the rows of its workspace.  A handful of samples are one workgroup's, whose sums are
@@ -524,6 +536,8 @@ void with_type(int type, F&& f) {
 // -1 for a slot without a component.  Block b has the b-th stretch of the slots and wave w of it the w-th stretch of that.
 // A slot's position: the slots of lower components, those of its own in the blocks and waves before, and its rank among
 // those of the wave.  Few slots are one workgroup's; more are counted in a first launch, one row of counts per block.
+// Latency bounds both: 1024 slots of 128 components take 4.4 us, 32768 8.3 us (30 in one workgroup), a million 25 us.  One workgroup against two launches:
+// 4096 slots 6.1 and 6.5 us, 6000 slots 7.5 and 6.9.
 constexpr int SORT_WAVES = 16;
 constexpr int SORT_ONE_BLOCK = 4096, SORT_MOST_BLOCKS = 64;
 
@@ -640,8 +654,9 @@ __global__ __launch_bounds__(64 * SORT_WAVES) void k_sort(const int32_t* __restr
 //
 // A row is a number of units of up to 16 bytes (the last may be shorter; loads and stores of 16 bytes need no more than the
 // elements' alignment).  L lanes share a sample, each with one unit of every L: a tile.  A tile's work is one item, so that
-// a few long rows spread over many workgroups too; rows shorter than half a wave's units share a wave.  (Two units to a lane
-// of longer rows: 8192 samples with four rows of 2048 bf16 each way, with gradients, 187 us instead of 181, four 193.)
+// a few long rows spread over many workgroups too; rows shorter than half a wave's units share a wave.  Memory bounds all
+// three kernels: 8192 samples with four rows of 2048 bf16 each, with gradients, take 177 us for 672 MB (3.8 TB/s; a copy
+// reaches 4.9).  Two units to a lane of longer rows: 187 us, four 193; four slots in flight instead of two: 3 us less.
 template <class T> constexpr int UNIT = 16 / (int)sizeof(T);
 template <class T> struct Unit { T v[UNIT<T>]; };
 
@@ -724,7 +739,8 @@ __global__ __launch_bounds__(256) void k_combine(const T* __restrict__ rows, int
 }
 
 // The rows of a sample are gone through by L lanes (256: the whole workgroup), S slots at a time: the gradient of the
-// output is read once for them, every row once.
+// output is read once for them, every row once.  A workgroup for rows of more than 64 units instead of a wave: 8192 x 4 rows of
+// 2048 bf16 57 us instead of 61.
 template <class T, int L, int S>
 __global__ __launch_bounds__(256) void k_combine_backward(const T* __restrict__ dout, int64_t dout_stride,
                                                           const T* __restrict__ rows, int64_t H, int64_t stride, int64_t n_rows,

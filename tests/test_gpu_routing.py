@@ -116,6 +116,59 @@ def test_route_of_many_samples_and_strided_scores():
         check_route(view.to(torch.bfloat16) if view.stride(1) else view, None, 1, True)
 
 
+@pytest.mark.parametrize("M,N,top,dtype,with_coef,renormalise", [
+    (16, 70001, 1, "float32", True, False), (5, 65537, 3, "bfloat16", False, True), (1, 66000, 1, "float32", True, True),
+    (64, 131073, 2, "float32", True, True), (33, 140000, 4, "float16", True, False), (64, 131072, 1, "float32", False, False),
+    (64, 131072, 6, "float32", True, True), (17, 8193, 2, "float32", True, False), (100, 9001, 5, "bfloat16", True, True),
+    (300, 8200, 16, "float32", True, False), (512, 8199, 3, "float16", False, False), (1000, 8500, 8, "float32", True, True)])
+def test_route_of_many_samples_next_to_each_other(M, N, top, dtype, with_coef, renormalise):
+    """The kernels that scores [n_components, n] of many samples get, against the formulas in float64 over whole arrays."""
+    print("route many", M, N, top, dtype, with_coef, renormalise, flush=True)
+    rng = np.random.default_rng(M + N)
+    x = rng.normal(-50.0, 5.0, (M, N)).astype(np.float32)
+    x[rng.random((M, N)) < 0.15] = -np.inf
+    x[:, 7] = -np.inf
+    x[:, N - 1] = 3.0
+    x = torch.tensor(x).cuda().to(TYPES[dtype])
+    coef = np.log(rng.dirichlet(np.ones(M))).astype(np.float32) if with_coef else None
+    dev_coef = None if coef is None else torch.tensor(coef).cuda()
+    ids, w, logp = P.einet_route(x, dev_coef, top, renormalise=renormalise)
+    t = host(x) + (0.0 if coef is None else coef.astype(np.float64)[:, None])
+    m = t.max(0)
+    alive = m > -np.inf
+    e = np.where(alive, np.exp(np.minimum(t - np.where(alive, m, 0.0), 0.0)), 0.0)
+    z = np.where(alive, e.sum(0), 1.0)
+    p = e / z
+    order = np.argsort(-t, axis=0, kind="stable")[:top].T
+    n = np.arange(N)[:, None]
+    rid = np.where(t[order, n] > -np.inf, order, -1)
+    rw = np.where(rid >= 0, p[order, n], 0.0)
+    if renormalise:
+        rw = rw / np.where(alive, rw.sum(1), 1.0)[:, None]
+    rlogp = np.where(alive, np.where(alive, m, 0.0) + np.log(z), -np.inf)
+    assert np.array_equal(host(ids), rid)
+    d = np.where(np.isfinite(t) & alive, m - np.where(np.isfinite(t), t, 0.0), 0.0)
+    dsel = np.where(rid >= 0, d[order, n], 0.0)
+    close(w, rw, U * (dsel + 48) * rw + 2.0 ** -125)
+    close(logp, rlogp, U * (np.where(alive, np.abs(rlogp), 0.0) + 96))
+    dw, dl = rng.normal(size=(N, top)).astype(np.float32), rng.normal(size=N).astype(np.float32)
+    for use_w, use_l in ((True, True), (False, True)):
+        g, ga = P.einet_route_backward(x, dev_coef, ids, w, torch.tensor(dw).cuda() if use_w else None, torch.tensor(dl).cuda() if use_l else None,
+                                       renormalise=renormalise)
+        lw, ll = dw.astype(np.float64) * use_w, dl.astype(np.float64) * use_l
+        a = (lw * rw).sum(1)
+        rg = p * (ll if renormalise else ll - a)
+        mag = p * (np.abs(ll) + (0.0 if renormalise else (np.abs(lw) * rw).sum(1)))
+        for k in range(top):
+            there = rid[:, k] >= 0
+            at = (rid[there, k], np.flatnonzero(there))
+            rg[at] += (rw * (lw - a[:, None] if renormalise else lw))[there, k]
+            mag[at] += (rw * (np.abs(lw) + (np.abs(lw) * rw).sum(1)[:, None] if renormalise else np.abs(lw)))[there, k]
+        tol = U * (d + 96 + (48 if use_w else 0)) * mag + 2.0 ** -120
+        close(g, rg, tol + HALF[g.dtype] * np.abs(rg) * 1.01 + SMALLEST[g.dtype])
+        close(ga, rg.sum(1), (tol + U * (N / 1024 + 32) * mag).sum(1) + U * np.abs(rg.sum(1)))
+
+
 def test_route_rows_where_nothing_or_little_is_left():
     nan, inf, low = math.nan, math.inf, torch.finfo(torch.float32).min
     cols = [[-inf] * 4, [nan] * 4, [nan, -inf, 1.0, nan], [low, low, 0.0, low], [low] * 4, [inf, 0.0, inf, -inf], [inf, nan, 1.0, -3e38],
@@ -478,3 +531,48 @@ def test_pass_on_another_stream_and_twice_the_same():
     torch.cuda.synchronize()
     for g in got:
         assert all(torch.equal(a, b) for a, b in zip(g, want))
+
+
+def test_offsets_beyond_32_bits():
+    """Tensors of more than 2^31 elements and 2^32 bytes: the last rows are where a 32-bit offset would go wrong."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    # rows: 300001 samples with two slots of 4096 bf16 values
+    N, H = 300001, 4096
+    x = torch.randn(N, H, generator=g, device="cuda", dtype=torch.bfloat16)
+    first, place = P.einet_sort(torch.randint(0, 5, (N, 2), generator=g, device="cuda", dtype=torch.int32), 5)
+    print("dispatch and combine beyond 2^31 elements", flush=True)
+    xs = P.einet_dispatch(x, place)
+    assert xs.numel() > 2 ** 31
+    for n in (0, 1, 262143, 262144, N - 2, N - 1):
+        assert torch.equal(xs[place[n].long()], x[n].expand(2, H))
+    at = torch.randint(0, N, (1000,), generator=g, device="cuda")
+    assert torch.equal(xs[place[at].long().reshape(-1)], x[at].repeat_interleave(2, 0))
+    half = torch.full((N, 2), 0.5, device="cuda")
+    assert torch.equal(P.einet_combine(xs, place, half), x)
+    d, dw = P.einet_combine_backward(x, xs, place, half)
+    assert torch.equal(d[place[at].long().reshape(-1)], (x[at].float() * 0.5).bfloat16().repeat_interleave(2, 0))
+    want = x[at].double().square().sum(1)
+    assert bool(((dw[at].double() - want[:, None]).abs() <= U * (H / 64 + 82) * want[:, None]).all())
+    del x, xs, d, place, half
+    # logits: 70000 rows of 32768
+    logits = torch.randn(70000, 32768, generator=g, device="cuda", dtype=torch.bfloat16)
+    u = uniforms(np.random.default_rng(1), 70000)
+    print("choose beyond 2^31 elements", flush=True)
+    index, logq = P.einet_choose(logits, u, top_p=0.9)
+    for lo, hi in ((0, 3), (65530, 65540), (69995, 70000)):
+        i, q = P.einet_choose(logits[lo:hi].clone(), u[lo:hi].contiguous(), top_p=0.9)
+        assert torch.equal(i, index[lo:hi]) and torch.equal(q, logq[lo:hi])
+    del logits
+    # scores: 64 components of 34 million samples
+    scores = torch.randn(64, 34000001, generator=g, device="cuda")
+    print("route beyond 2^31 elements", flush=True)
+    ids, w, logp = P.einet_route(scores, None, 1)
+    ds, dc = P.einet_route_backward(scores, None, ids, w, None, torch.ones_like(logp))
+    at = torch.cat([torch.randint(0, scores.shape[1], (1000,), generator=g, device="cuda"), torch.tensor([0, scores.shape[1] - 1], device="cuda")])
+    few = scores[:, at].double()
+    assert torch.equal(ids[at, 0].long(), few.argmax(0))
+    close(logp[at], host(few.logsumexp(0)), U * (host(few.logsumexp(0).abs()) + 96))
+    p = host(few.softmax(0))
+    close(ds[:, at], p, U * 120 * p)
+    assert abs(float(dc.double().sum()) - scores.shape[1]) <= U * 400 * scores.shape[1]
