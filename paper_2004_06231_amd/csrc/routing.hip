@@ -500,11 +500,14 @@ bool route_staged(const Scores& a) { return a.sn == 1 && a.sc != 1 && a.M > 16 &
 template <int G> size_t route_tile_bytes(int M) { return sizeof(float) * ROUTE_STAGE<G> * (size_t)(M | 1); }
 
 // Workgroups of the gradient, which is the rows of its workspace.  A handful of samples are one workgroup's, whose sums are
-// the gradient of the coefficients: no second launch and no workspace.
-int route_backward_groups(int M, int64_t N) {
+// the gradient of the coefficients: no second launch and no workspace.  Two to a compute unit, four where many samples are read
+// directly: the loads of a wave's next samples wait for its last ones there (262144 rows of 64: 35 us instead of 54, 100000 of 128
+// 25 instead of 35; through LDS 262144 x 100 took 103 instead of 98).
+int route_backward_groups(int M, int64_t N, bool directly) {
     if (N <= (M <= 64 ? 32 : 8)) return 1;
     const int64_t tiles = (N + 3) / 4;               // (a workgroup has four samples at least)
-    return (int)(tiles < 2 * EINET_NUM_CUS ? tiles : 2 * EINET_NUM_CUS);
+    const int most = (directly && N >= 256 * EINET_NUM_CUS ? 4 : 2) * EINET_NUM_CUS;
+    return (int)(tiles < most ? tiles : most);
 }
 
 // f(std::integral_constant<int, G>, std::integral_constant<int, E>) for the lanes and components per lane of M, top
@@ -868,14 +871,15 @@ void launch_route(const Scores& a, int top, bool renormalise, int32_t* ids, floa
 }
 
 size_t route_backward_workspace(int M, int64_t N) {
-    const int groups = route_backward_groups(M, N);
+    const int groups = route_backward_groups(M, N, true);
     return groups > 1 ? sizeof(float) * (size_t)groups * M : 0;
 }
 
 void launch_route_backward(const Scores& a, int top, bool renormalise, const int32_t* ids, const float* weights,
                            const float* dweights, const float* dlogp, void* dscores, int64_t dsc, int64_t dsn, float* dcoef,
                            void* workspace, hipStream_t s) {
-    const int groups = route_backward_groups(a.M, a.N), re = renormalise ? 1 : 0;
+    const bool by_columns = route_by_columns(a, top) && dsn == 1, staged_rows = route_staged(a) && dsn == 1;
+    const int groups = route_backward_groups(a.M, a.N, !by_columns && !staged_rows), re = renormalise ? 1 : 0;
     float* const partial = !dcoef ? nullptr : groups > 1 ? static_cast<float*>(workspace) : dcoef;
     if (a.N > 0)
         route_types(a, [&](auto t, auto k) {
@@ -883,7 +887,7 @@ void launch_route_backward(const Scores& a, int top, bool renormalise, const int
             using K = decltype(k);
             const T* const p = static_cast<const T*>(a.p);
             T* const d = static_cast<T*>(dscores);
-            if (route_by_columns(a, top) && dsn == 1) {
+            if (by_columns) {
                 columns_variant(a.M, top, [&](auto most, auto components) {
                     hipLaunchKernelGGL((k_route_backward_columns<T, K, decltype(most)::value, decltype(components)::value>), dim3(groups),
                                        dim3(256), 0, s, p, a.sc, a.coef, a.M, a.N, top, re, ids, weights, dweights, dlogp, d, dsc, partial);
@@ -898,7 +902,7 @@ void launch_route_backward(const Scores& a, int top, bool renormalise, const int
                                        STAGED ? route_tile_bytes<G>(a.M) : 0, s, p, a.sc, a.sn, a.coef, a.M, a.N, top, re, ids, weights,
                                        dweights, dlogp, d, dsc, dsn, partial);
                 };
-                if (route_staged(a) && dsn == 1) go(std::true_type{});
+                if (staged_rows) go(std::true_type{});
                 else go(std::false_type{});
             });
         });
