@@ -26,6 +26,7 @@ int check_hip(const char* call) {
 bool known_type(int t) { return t == EINET_FLOAT32 || t == EINET_BFLOAT16 || t == EINET_FLOAT16; }
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 constexpr int64_t MOST_SLOTS = 0x7fffffff;
+const char* const MISALIGNED = "a pointer is not aligned to its elements";
 
 const char* route_problem(const void* score, int dtype, int64_t sc, int64_t sn, const float* coef, int M, int64_t n, int top) {
     if (!known_type(dtype)) return "unknown dtype";
@@ -34,7 +35,7 @@ const char* route_problem(const void* score, int dtype, int64_t sc, int64_t sn, 
     if (n < 0 || n > MOST_SLOTS / top) return "n must be at least 0 and n * top below 2^31";
     if (sc < 0 || sn < 0) return "strides must not be negative";
     if (!score && n > 0) return "score_dev is NULL";
-    if (!aligned(score, row_type_bytes(dtype)) || !aligned(coef, 4)) return "a pointer is not aligned to its elements";
+    if (!aligned(score, row_type_bytes(dtype)) || !aligned(coef, 4)) return MISALIGNED;
     return nullptr;
 }
 
@@ -58,7 +59,7 @@ int einet_route(const void* score_dev, int dtype, int64_t component_stride, int6
         return invalid(call, e);
     if (n == 0) return EINET_OK;
     if (!id_dev || !weight_dev || !logp_dev) return invalid(call, "NULL pointer");
-    if (!aligned(id_dev, 4) || !aligned(weight_dev, 4) || !aligned(logp_dev, 4)) return invalid(call, "a pointer is not aligned to its elements");
+    if (!aligned(id_dev, 4) || !aligned(weight_dev, 4) || !aligned(logp_dev, 4)) return invalid(call, MISALIGNED);
     launch_route(Scores{score_dev, dtype, component_stride, sample_stride, log_coef_dev, n_components, n}, top, renormalise != 0,
                  id_dev, weight_dev, logp_dev, static_cast<hipStream_t>(stream));
     return check_hip(call);
@@ -83,7 +84,7 @@ int einet_route_backward(const void* score_dev, int dtype, int64_t component_str
     if (n > 0 && (!dscore_dev || (dweight_dev && (!id_dev || !weight_dev)))) return invalid(call, "NULL pointer");
     if (!aligned(dscore_dev, row_type_bytes(dtype)) || !aligned(id_dev, 4) || !aligned(weight_dev, 4) || !aligned(dweight_dev, 4) ||
         !aligned(dlogp_dev, 4) || !aligned(dlog_coef_dev, 4))
-        return invalid(call, "a pointer is not aligned to its elements");
+        return invalid(call, MISALIGNED);
     const size_t need = route_backward_workspace(n_components, n);
     if (dlog_coef_dev && need > 0 && (!workspace_dev || !aligned(workspace_dev, 16) || workspace_bytes < need))
         return invalid(call, "dlog_coef_dev needs a workspace of einet_route_workspace bytes, 16-byte aligned");
@@ -107,7 +108,7 @@ int einet_sort(const int32_t* id_dev, int64_t n_slots, int n_components, int32_t
         return invalid(call, "n_components must be in 1..EINET_ROUTE_MAX_COMPONENTS");
     if (n_slots < 0 || n_slots > MOST_SLOTS) return invalid(call, "n_slots must be in 0..2^31-1");
     if (!first_dev || (n_slots > 0 && (!id_dev || !place_dev))) return invalid(call, "NULL pointer");
-    if (!aligned(id_dev, 4) || !aligned(first_dev, 4) || !aligned(place_dev, 4)) return invalid(call, "a pointer is not aligned to its elements");
+    if (!aligned(id_dev, 4) || !aligned(first_dev, 4) || !aligned(place_dev, 4)) return invalid(call, MISALIGNED);
     const size_t need = sort_workspace(n_slots, n_components);
     if (need > 0 && (!workspace_dev || !aligned(workspace_dev, 16) || workspace_bytes < need))
         return invalid(call, "needs a workspace of einet_sort_workspace bytes, 16-byte aligned");
@@ -123,7 +124,7 @@ int einet_dispatch(const void* row_dev, int64_t row_bytes, int64_t row_stride_by
     if (out_stride_bytes < row_bytes) return invalid(call, "rows of out_dev would overlap");
     if (n == 0 || row_bytes == 0 || out_rows == 0) return EINET_OK;
     if (!row_dev || !place_dev || !out_dev) return invalid(call, "NULL pointer");
-    if (!aligned(place_dev, 4)) return invalid(call, "a pointer is not aligned to its elements");
+    if (!aligned(place_dev, 4)) return invalid(call, MISALIGNED);
     launch_dispatch(row_dev, row_bytes, row_stride_bytes, n, top, place_dev, out_dev, out_stride_bytes, out_rows,
                     static_cast<hipStream_t>(stream));
     return check_hip(call);
@@ -140,7 +141,7 @@ int einet_combine(const void* row_dev, int dtype, int64_t width, int64_t row_str
     if ((!row_dev && n_rows > 0) || !place_dev || !out_dev) return invalid(call, "NULL pointer");
     const size_t e = row_type_bytes(dtype);
     if (!aligned(row_dev, e) || !aligned(out_dev, e) || !aligned(place_dev, 4) || !aligned(weight_dev, 4))
-        return invalid(call, "a pointer is not aligned to its elements");
+        return invalid(call, MISALIGNED);
     launch_combine(row_dev, dtype, width, row_stride, n_rows, place_dev, weight_dev, n, top, out_dev, out_stride,
                    static_cast<hipStream_t>(stream));
     return check_hip(call);
@@ -160,7 +161,7 @@ int einet_combine_backward(const void* dout_dev, int64_t dout_stride, const void
     const size_t e = row_type_bytes(dtype);
     if (!aligned(dout_dev, e) || !aligned(row_dev, e) || !aligned(drow_dev, e) || !aligned(place_dev, 4) || !aligned(weight_dev, 4) ||
         !aligned(dweight_dev, 4))
-        return invalid(call, "a pointer is not aligned to its elements");
+        return invalid(call, MISALIGNED);
     launch_combine_backward(dout_dev, dout_stride, row_dev, dtype, width, row_stride, n_rows, place_dev, weight_dev, n, top, drow_dev,
                             drow_stride, dweight_dev, static_cast<hipStream_t>(stream));
     return check_hip(call);
@@ -190,7 +191,7 @@ int einet_choose(const void* logit_dev, int dtype, int64_t row_stride, int n_row
     if (!logit_dev || !u_dev || !index_dev) return invalid(call, "NULL pointer");
     if (!aligned(logit_dev, row_type_bytes(dtype)) || !aligned(u_dev, 4) || !aligned(temperature_dev, 4) || !aligned(top_k_dev, 4) ||
         !aligned(top_p_dev, 4) || !aligned(min_p_dev, 4) || !aligned(index_dev, 4) || !aligned(logq_dev, 4))
-        return invalid(call, "a pointer is not aligned to its elements");
+        return invalid(call, MISALIGNED);
     const size_t need = choose_workspace(n_rows, n_entries);
     if (need > 0 && (!workspace_dev || !aligned(workspace_dev, 256) || workspace_bytes < need))
         return invalid(call, "needs a workspace of einet_choose_workspace bytes, 256-byte aligned");

@@ -67,9 +67,10 @@ __device__ __forceinline__ RowSettings row_settings(const ChooseArgs& a, int row
     return s;
 }
 
-// 2^y in units of 2^-shift, shift <= 61, rounded to the nearest, for y <= 0 (0 for NaN).  2^y = 2^n 2^f with n the nearest integer: the
-// series of 2^f = exp(f ln 2) to the 12th power is good to 0.347^13 / 13! = 1.7e-16.  Added to 2 its last place is 2^-51,
-// whole.  (The coefficients are kept in scalar registers: as literals each takes two moves before its multiplication.)
+// 2^y in units of 2^-shift, shift <= 61, rounded to the nearest, for y <= 0 (0 for NaN).  2^y = 2^n 2^f with n the nearest
+// integer: the series of 2^f = exp(f ln 2) to the 12th power is good to 0.347^13 / 13! = 1.7e-16.  Added to 2 its last place
+// is 2^-51, whole.  (The coefficients are kept in scalar registers: as literals each takes two moves before its
+// multiplication.)
 __device__ __forceinline__ double scalar_constant(double c) {
     asm("" : "+s"(c));
     return c;
@@ -770,7 +771,8 @@ struct SplitRow {
 
 // the part's entries as RowLogits; index 0 of them is entry `origin` of the row
 template <class T>
-__device__ __forceinline__ int split_part(const ChooseArgs& a, const SplitRows& sp, int row, int part, RowLogits<T, SPLIT_THREADS, 0>& keys) {
+__device__ __forceinline__ int split_part(const ChooseArgs& a, const SplitRows& sp, int row, int part,
+                                          RowLogits<T, SPLIT_THREADS, 0>& keys) {
     const int origin = part * sp.per;
     keys.init(static_cast<const T*>(a.logits) + row * a.stride + origin, min(sp.per, a.V - origin));
     keys.groups = sp.per / (4 * SPLIT_THREADS);                  // (of a whole part, also in a shorter last one)

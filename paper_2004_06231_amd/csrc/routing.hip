@@ -135,9 +135,9 @@ __device__ __forceinline__ K staged_load(const float* tile, const float* __restr
 }
 
 template <class T, class K, int G, int E, bool STAGED>
-__global__ __launch_bounds__((ROUTE_THREADS<G, STAGED>)) void k_route(const T* __restrict__ p, int64_t sc, int64_t sn, const float* __restrict__ coef,
-                                               int M, int64_t N, int top, int renormalise, int32_t* __restrict__ ids,
-                                               float* __restrict__ weights, float* __restrict__ logp) {
+__global__ __launch_bounds__((ROUTE_THREADS<G, STAGED>))
+void k_route(const T* __restrict__ p, int64_t sc, int64_t sn, const float* __restrict__ coef, int M, int64_t N, int top,
+             int renormalise, int32_t* __restrict__ ids, float* __restrict__ weights, float* __restrict__ logp) {
     constexpr int S = ROUTE_THREADS<G, STAGED> / G;
     const int j = threadIdx.x % G;
     const int64_t n = (int64_t)blockIdx.x * S + threadIdx.x / G;
@@ -372,13 +372,15 @@ __device__ __forceinline__ float fold_lanes(float (&d)[MOST]) {
     if constexpr (MOST == 64) {
 #pragma unroll
         for (int c = 0; c < 32; ++c) {
-            const auto v = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, d[c]), __builtin_bit_cast(uint32_t, d[c + 32]), false, false);
+            const uint32_t a = __builtin_bit_cast(uint32_t, d[c]), b = __builtin_bit_cast(uint32_t, d[c + 32]);
+            const auto v = __builtin_amdgcn_permlane32_swap(a, b, false, false);
             const uint32_t v0 = v[0], v1 = v[1];
             d[c] = __builtin_bit_cast(float, v0) + __builtin_bit_cast(float, v1);
         }
 #pragma unroll
         for (int c = 0; c < 16; ++c) {
-            const auto v = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, d[c]), __builtin_bit_cast(uint32_t, d[c + 16]), false, false);
+            const uint32_t a = __builtin_bit_cast(uint32_t, d[c]), b = __builtin_bit_cast(uint32_t, d[c + 16]);
+            const auto v = __builtin_amdgcn_permlane16_swap(a, b, false, false);
             const uint32_t v0 = v[0], v1 = v[1];
             d[c] = __builtin_bit_cast(float, v0) + __builtin_bit_cast(float, v1);
         }
@@ -539,8 +541,8 @@ void with_type(int type, F&& f) {
 // -1 for a slot without a component.  Block b has the b-th stretch of the slots and wave w of it the w-th stretch of that.
 // A slot's position: the slots of lower components, those of its own in the blocks and waves before, and its rank among
 // those of the wave.  Few slots are one workgroup's; more are counted in a first launch, one row of counts per block.
-// Latency bounds both: 1024 slots of 128 components take 4.4 us, 32768 8.3 us (30 in one workgroup), a million 25 us.  One workgroup against two launches:
-// 4096 slots 6.1 and 6.5 us, 6000 slots 7.5 and 6.9.
+// Latency bounds both: 1024 slots of 128 components take 4.4 us, 32768 8.3 us (30 in one workgroup), a million 25 us.
+// One workgroup against two launches: 4096 slots 6.1 and 6.5 us, 6000 slots 7.5 and 6.9.
 constexpr int SORT_WAVES = 16;
 constexpr int SORT_ONE_BLOCK = 4096, SORT_MOST_BLOCKS = 64;
 

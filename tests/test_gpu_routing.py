@@ -290,6 +290,25 @@ def test_rows_of_any_type_and_shape_are_carried():
     assert d.shape == (74, 0) and not bool(dw.any())
 
 
+def test_batches_and_rows_of_length_zero():
+    dev = dict(device="cuda")
+    scores = torch.zeros(5, 0, **dev)
+    ids, w, logp = P.einet_route(scores, torch.zeros(5, **dev), 3)
+    assert ids.shape == (0, 3) and w.shape == (0, 3) and logp.shape == (0,)
+    g, ga = P.einet_route_backward(scores, None, ids, w, w, logp)
+    assert g.shape == (5, 0) and ga.tolist() == [0.0] * 5
+    first, place = P.einet_sort(torch.zeros(0, 2, dtype=torch.int32, **dev), 3)
+    assert first.tolist() == [0] * 4 and place.shape == (0, 2)
+    # no sorted rows: every slot goes nowhere
+    nowhere = torch.full((4, 2), -1, dtype=torch.int32, **dev)
+    assert not bool(P.einet_combine(torch.empty(0, 6, **dev), nowhere, torch.ones(4, 2, **dev)).any())
+    d, dw = P.einet_combine_backward(torch.ones(4, 6, **dev), torch.empty(0, 6, **dev), nowhere, torch.ones(4, 2, **dev))
+    assert d.shape == (0, 6) and not bool(dw.any())
+    assert P.einet_dispatch(torch.ones(4, 6, **dev), nowhere, out=torch.empty(0, 6, **dev)).shape == (0, 6)
+    with pytest.raises(P.EinetError):
+        P.einet_choose(torch.zeros(3, 0, **dev), torch.zeros(3, **dev))
+
+
 def test_positions_out_of_range_go_nowhere():
     place = torch.tensor([[0, 99], [-7, 3], [2 ** 31 - 1, -1]], dtype=torch.int32, device="cuda")
     x = torch.arange(24.0, device="cuda").reshape(3, 8)
