@@ -354,7 +354,8 @@ int einet_route_workspace(int n_components, int64_t n, size_t* bytes);
  *   dscore_dev     device, written completely, of `dtype`, entry (c, i) at c * dcomponent_stride + i * dsample_stride
  *   dlog_coef_dev  device, [n_components] float32, written, or NULL; needs the workspace (einet_route_workspace bytes,
  *                  16-byte aligned; NULL if that is 0)
- * The entries of dscore_dev must share no memory with each other nor with an input.  n = 0 writes zeros to dlog_coef_dev.  Errors as einet_route. */
+ * The entries of dscore_dev must share no memory with each other nor with an input.  n = 0 writes zeros to dlog_coef_dev.
+ * Errors as einet_route. */
 int einet_route_backward(const void* score_dev, int dtype, int64_t component_stride, int64_t sample_stride,
                          const float* log_coef_dev, int n_components, int64_t n, int top, int renormalise,
                          const int32_t* id_dev, const float* weight_dev, const float* dweight_dev, const float* dlogp_dev,
@@ -382,7 +383,8 @@ int einet_sort(const int32_t* id_dev, int64_t n_slots, int n_components, int32_t
  *   row_dev    device, row i at i * row_stride_bytes (0: the same row for all);  place_dev  device, [n][top] int32
  *   out_dev    device, row p at p * out_stride_bytes
  * The gradient of row is einet_combine of the gradient of out without weights.  Errors: EINET_ERR_INVALID_ARG (top < 1, n < 0,
- * n * top above 2^31 - 1, negative sizes, out_stride_bytes < row_bytes, NULL pointers), EINET_ERR_HIP. */
+ * n * top above 2^31 - 1, negative sizes, a row of more than 2^35 bytes, out_stride_bytes < row_bytes, NULL pointers),
+ * EINET_ERR_HIP. */
 int einet_dispatch(const void* row_dev, int64_t row_bytes, int64_t row_stride_bytes, int64_t n, int top,
                    const int32_t* place_dev, void* out_dev, int64_t out_stride_bytes, int64_t out_rows, void* stream);
 
@@ -390,7 +392,7 @@ int einet_dispatch(const void* row_dev, int64_t row_bytes, int64_t row_stride_by
  * 0..n_rows-1 (zeros where there is none), summed in float32 in the order of the slots and rounded once.
  *   row_dev     device, [n_rows][width] of `dtype`, rows row_stride elements apart
  *   place_dev   device, [n][top] int32;  weight_dev  device, [n][top] float32, or NULL: all one
- *   out_dev     device, [n][width] of `dtype`, rows out_stride elements apart, written completely
+ *   out_dev     device, [n][width] of `dtype`, rows out_stride elements apart, written completely; must not overlap row_dev
  * Errors as einet_dispatch, and unknown dtype. */
 int einet_combine(const void* row_dev, int dtype, int64_t width, int64_t row_stride, int64_t n_rows,
                   const int32_t* place_dev, const float* weight_dev, int64_t n, int top, void* out_dev, int64_t out_stride,

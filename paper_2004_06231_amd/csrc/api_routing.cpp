@@ -40,10 +40,11 @@ const char* route_problem(const void* score, int dtype, int64_t sc, int64_t sn, 
 }
 
 // what the calls that carry rows have in common
-const char* slots_problem(int64_t n, int top, int64_t n_rows) {
+const char* slots_problem(int64_t n, int top, int64_t n_rows, int64_t width, int64_t element_bytes) {
     if (top < 1) return "top must be at least 1";
     if (n < 0 || n > MOST_SLOTS / top) return "n must be at least 0 and n * top below 2^31";
     if (n_rows < 0) return "the number of sorted rows must not be negative";
+    if (width > ROW_MOST_BYTES / element_bytes) return "a row must not have more than 2^35 bytes";
     return nullptr;
 }
 
@@ -119,7 +120,7 @@ int einet_sort(const int32_t* id_dev, int64_t n_slots, int n_components, int32_t
 int einet_dispatch(const void* row_dev, int64_t row_bytes, int64_t row_stride_bytes, int64_t n, int top, const int32_t* place_dev,
                    void* out_dev, int64_t out_stride_bytes, int64_t out_rows, void* stream) {
     const char* const call = "einet_dispatch";
-    if (const char* e = slots_problem(n, top, out_rows)) return invalid(call, e);
+    if (const char* e = slots_problem(n, top, out_rows, row_bytes, 1)) return invalid(call, e);
     if (row_bytes < 0 || row_stride_bytes < 0) return invalid(call, "row_bytes and the strides must not be negative");
     if (out_stride_bytes < row_bytes) return invalid(call, "rows of out_dev would overlap");
     if (n == 0 || row_bytes == 0 || out_rows == 0) return EINET_OK;
@@ -134,7 +135,7 @@ int einet_combine(const void* row_dev, int dtype, int64_t width, int64_t row_str
                   const float* weight_dev, int64_t n, int top, void* out_dev, int64_t out_stride, void* stream) {
     const char* const call = "einet_combine";
     if (!known_type(dtype)) return invalid(call, "unknown dtype");
-    if (const char* e = slots_problem(n, top, n_rows)) return invalid(call, e);
+    if (const char* e = slots_problem(n, top, n_rows, width, row_type_bytes(dtype))) return invalid(call, e);
     if (width < 0 || row_stride < 0) return invalid(call, "width and the strides must not be negative");
     if (out_stride < width) return invalid(call, "rows of out_dev would overlap");
     if (n == 0 || width == 0) return EINET_OK;
@@ -152,7 +153,7 @@ int einet_combine_backward(const void* dout_dev, int64_t dout_stride, const void
                            void* drow_dev, int64_t drow_stride, float* dweight_dev, void* stream) {
     const char* const call = "einet_combine_backward";
     if (!known_type(dtype)) return invalid(call, "unknown dtype");
-    if (const char* e = slots_problem(n, top, n_rows)) return invalid(call, e);
+    if (const char* e = slots_problem(n, top, n_rows, width, row_type_bytes(dtype))) return invalid(call, e);
     if (width < 0 || row_stride < 0 || dout_stride < 0) return invalid(call, "width and the strides must not be negative");
     if (drow_stride < width) return invalid(call, "rows of drow_dev would overlap");
     if (n == 0) return EINET_OK;

@@ -1052,19 +1052,24 @@ void launch_choose_split(const ChooseArgs& a, const SplitRows& sp, int shift, hi
 template <class T>
 void launch_choose_rows(const ChooseArgs& a, int shift, hipStream_t s) {
     const int V = a.V;
-    const dim3 waves((a.B + 3) / 4), rows(a.B);
+    // `threads` to a workgroup, which has `per` rows
+    auto go = [&](auto kernel, int threads, int per) {
+        row_batches(a.B, threads / per, [&](int64_t b0, int64_t b) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((b + per - 1) / per)), dim3(threads), 0, s, rows_from(a, (int)b0, (int)b), shift);
+        });
+    };
     SplitRows sp;
-    if (V <= 64) hipLaunchKernelGGL((k_choose_wave<T, 1, 1>), waves, dim3(256), 0, s, a, shift);
-    else if (V <= 128) hipLaunchKernelGGL((k_choose_wave<T, 2, 1>), waves, dim3(256), 0, s, a, shift);
-    else if (V <= 256) hipLaunchKernelGGL((k_choose_wave<T, 4, 1>), waves, dim3(256), 0, s, a, shift);
-    else if (V <= 512) hipLaunchKernelGGL((k_choose_wave<T, 4, 2>), waves, dim3(256), 0, s, a, shift);
-    else if (V <= 1024) hipLaunchKernelGGL((k_choose_wave<T, 4, 4>), waves, dim3(256), 0, s, a, shift);
-    else if (V <= 2048) hipLaunchKernelGGL((k_choose_block<T, 256, 2>), rows, dim3(256), 0, s, a, shift);
-    else if (V <= 4096) hipLaunchKernelGGL((k_choose_block<T, 512, 2>), rows, dim3(512), 0, s, a, shift);
-    else if (split_layout(a.B, V, static_cast<char*>(a.workspace), sp) == 0)
-        hipLaunchKernelGGL((k_choose_block<T, 1024, 2>), rows, dim3(1024), 0, s, a, shift);
+    if (V <= 64) go(k_choose_wave<T, 1, 1>, 256, 4);
+    else if (V <= 128) go(k_choose_wave<T, 2, 1>, 256, 4);
+    else if (V <= 256) go(k_choose_wave<T, 4, 1>, 256, 4);
+    else if (V <= 512) go(k_choose_wave<T, 4, 2>, 256, 4);
+    else if (V <= 1024) go(k_choose_wave<T, 4, 4>, 256, 4);
+    else if (V <= 2048) go(k_choose_block<T, 256, 2>, 256, 1);
+    else if (V <= 4096) go(k_choose_block<T, 512, 2>, 512, 1);
+    else if (split_layout(a.B, V, static_cast<char*>(a.workspace), sp) == 0) go(k_choose_block<T, 1024, 2>, 1024, 1);
     else
-        for (int b0 = 0; b0 < a.B; b0 += SPLIT_ROWS) launch_choose_split<T>(rows_from(a, b0, min(a.B - b0, SPLIT_ROWS)), sp, shift, s);
+        for (int64_t b0 = 0; b0 < a.B; b0 += SPLIT_ROWS)
+            launch_choose_split<T>(rows_from(a, (int)b0, min(a.B - (int)b0, SPLIT_ROWS)), sp, shift, s);
 }
 
 }  // namespace

@@ -687,7 +687,7 @@ __device__ __forceinline__ void store_unit(T* p, int64_t left, const Unit<T>& u)
 // The item of a lane: its sample and the column of its unit.
 template <class T, int L>
 __device__ __forceinline__ bool row_item(int64_t N, int64_t H, int tiles, int64_t& n, int64_t& k) {
-    uint32_t item = blockIdx.x * (256 / L) + threadIdx.x / L;        // (N * tiles < 2^31: seen to by the launcher)
+    uint32_t item = blockIdx.x * (256 / L) + threadIdx.x / L;        // (a launch has fewer than 2^32 lanes)
     if constexpr (L == 64) item = (uint32_t)__builtin_amdgcn_readfirstlane((int)item);
     const uint32_t i = tiles == 1 ? item : item / (uint32_t)tiles;
     n = i;
@@ -863,8 +863,11 @@ void launch_route(const Scores& a, int top, bool renormalise, int32_t* ids, floa
             auto go = [&](auto staged) {
                 constexpr bool STAGED = decltype(staged)::value;
                 constexpr int NT = ROUTE_THREADS<G, STAGED>, S = NT / G;
-                hipLaunchKernelGGL((k_route<T, K, G, E, STAGED>), dim3((unsigned)((a.N + S - 1) / S)), dim3(NT),
-                                   STAGED ? route_tile_bytes<G>(a.M) : 0, s, p, a.sc, a.sn, a.coef, a.M, a.N, top, re, ids, weights, logp);
+                row_batches(a.N, G, [&](int64_t n0, int64_t n) {
+                    hipLaunchKernelGGL((k_route<T, K, G, E, STAGED>), dim3((unsigned)((n + S - 1) / S)), dim3(NT),
+                                       STAGED ? route_tile_bytes<G>(a.M) : 0, s, p + n0 * a.sn, a.sc, a.sn, a.coef, a.M, n, top, re,
+                                       ids + n0 * top, weights + n0 * top, logp + n0);
+                });
             };
             if (route_staged(a)) go(std::true_type{});
             else go(std::false_type{});
@@ -928,13 +931,6 @@ void launch_sort(const int32_t* ids, int64_t slots, int M, int32_t* first, int32
     hipLaunchKernelGGL(k_sort, dim3(blocks), dim3(64 * SORT_WAVES), lds, s, ids, slots, M, bits, counts, first, place);
 }
 
-// Samples in launches of fewer than 2^31 items: f(first sample, samples).
-template <class F>
-void row_batches(int64_t N, int64_t tiles, F&& f) {
-    const int64_t most = std::max<int64_t>(0x7fffffff / tiles, 1);
-    for (int64_t n0 = 0; n0 < N; n0 += most) f(n0, std::min(N - n0, most));
-}
-
 void launch_dispatch(const void* x, int64_t row_bytes, int64_t x_stride, int64_t N, int top, const int32_t* place, void* out,
                      int64_t out_stride, int64_t out_rows, hipStream_t s) {
     if (N == 0 || row_bytes == 0 || out_rows == 0) return;
@@ -947,7 +943,7 @@ void launch_dispatch(const void* x, int64_t row_bytes, int64_t x_stride, int64_t
         row_lanes(units, [&](auto l) {
             constexpr int L = decltype(l)::value;
             const int64_t tiles = (units + L - 1) / L;
-            row_batches(N, tiles, [&](int64_t n0, int64_t n) {
+            row_batches(N, tiles * L, [&](int64_t n0, int64_t n) {
                 hipLaunchKernelGGL((k_dispatch<T, L>), dim3((unsigned)((n * tiles + 256 / L - 1) / (256 / L))), dim3(256), 0, s,
                                    static_cast<const T*>(x) + n0 * (x_stride / e), H, x_stride / e, n, (int)tiles, top,
                                    place + n0 * top, static_cast<T*>(out), out_stride / e, out_rows);
@@ -976,7 +972,7 @@ void launch_combine(const void* rows, int type, int64_t H, int64_t stride, int64
         row_lanes(units, [&](auto l) {
             constexpr int L = decltype(l)::value;
             const int64_t tiles = (units + L - 1) / L;
-            row_batches(N, tiles, [&](int64_t n0, int64_t n) {
+            row_batches(N, tiles * L, [&](int64_t n0, int64_t n) {
                 slots_together(top, [&](auto q) {
                     hipLaunchKernelGGL((k_combine<T, L, decltype(q)::value>), dim3((unsigned)((n * tiles + 256 / L - 1) / (256 / L))),
                                        dim3(256), 0, s, static_cast<const T*>(rows), H, stride, n_rows, place + n0 * top,
@@ -997,10 +993,13 @@ void launch_combine_backward(const void* dout, int64_t dout_stride, const void* 
         const int64_t units = (H + UNIT<T> - 1) / UNIT<T>;
         auto go = [&](auto l) {
             constexpr int L = decltype(l)::value;
-            slots_together(top, [&](auto q) {
-                hipLaunchKernelGGL((k_combine_backward<T, L, decltype(q)::value>), dim3((unsigned)((N + 256 / L - 1) / (256 / L))),
-                                   dim3(256), 0, s, static_cast<const T*>(dout), dout_stride, static_cast<const T*>(rows), H, stride,
-                                   n_rows, place, weights, N, top, static_cast<T*>(drows), drows_stride, dweights);
+            row_batches(N, L, [&](int64_t n0, int64_t n) {
+                slots_together(top, [&](auto q) {
+                    hipLaunchKernelGGL((k_combine_backward<T, L, decltype(q)::value>), dim3((unsigned)((n + 256 / L - 1) / (256 / L))),
+                                       dim3(256), 0, s, static_cast<const T*>(dout) + n0 * dout_stride, dout_stride,
+                                       static_cast<const T*>(rows), H, stride, n_rows, place + n0 * top, weights + n0 * top, n, top,
+                                       static_cast<T*>(drows), drows_stride, dweights + n0 * top);
+                });
             });
         };
         if (units > 64) go(std::integral_constant<int, 256>{});

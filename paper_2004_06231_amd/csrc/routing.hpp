@@ -5,6 +5,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstddef>
 #include <cstdint>
 
@@ -14,6 +15,15 @@ enum RowType { ROW_FLOAT32 = 0, ROW_BFLOAT16 = 1, ROW_FLOAT16 = 2 };      // EIN
 inline int row_type_bytes(int t) { return t == ROW_FLOAT32 ? 4 : 2; }
 
 constexpr int ROUTE_MAX_COMPONENTS = 1024, ROUTE_MAX_TOP = 16;
+
+// A launch holds fewer than 2^32 work-items: rows of `items` work-items each, in launches of as many rows as fit.
+// f(first row, rows)
+template <class F>
+void row_batches(int64_t rows, int64_t items, F&& f) {
+    const int64_t most = std::max<int64_t>((0xffffffffll - 1023) / items, 1);      // (1023: up to a whole workgroup)
+    for (int64_t r = 0; r < rows; r += most) f(r, std::min(rows - r, most));
+}
+constexpr int64_t ROW_MOST_BYTES = 1ll << 35;                                      // 2^31 units of 16 bytes
 
 // scores: entry (component c, sample n) at c * sc + n * sn
 struct Scores {

@@ -595,3 +595,51 @@ def test_offsets_beyond_32_bits():
     p = host(few.softmax(0))
     close(ds[:, at], p, U * 120 * p)
     assert abs(float(dc.double().sum()) - scores.shape[1]) <= U * 400 * scores.shape[1]
+
+
+def test_more_rows_than_a_launch_has_lanes_for():
+    """A launch holds fewer than 2^32 lanes: rows that are one row over and over need little memory and more lanes than that."""
+    B = 2 ** 26 + 5                                               # (64 lanes to a row)
+    u = torch.zeros(B, device="cuda")
+    tail = torch.tensor([0.0, 0.3, 0.6, 0.9, 0.99], device="cuda")
+    u[-5:] = tail
+    u[2 ** 26 - 16:2 ** 26 - 11] = tail
+    for V in (3, 700):
+        print("choose", B, V, flush=True)
+        row = torch.linspace(-1.0, 1.0, V, device="cuda")
+        index, logq = P.einet_choose(row.expand(B, V), u, top_p=0.95)
+        few, share = P.einet_choose(row.expand(5, V), tail, top_p=0.95)
+        for at in (slice(B - 5, B), slice(2 ** 26 - 16, 2 ** 26 - 11)):
+            assert torch.equal(index[at], few) and torch.equal(logq[at], share)
+        assert torch.equal(index[:2 ** 26 - 16], few[:1].expand(2 ** 26 - 16)) and torch.equal(index[2 ** 26 - 11:B - 5], few[:1].expand(11))
+    B = 2 ** 24 + 5                                               # (256 lanes to a row)
+    print("choose", B, 2000, flush=True)
+    row = torch.linspace(-1.0, 1.0, 2000, device="cuda")
+    index, logq = P.einet_choose(row.expand(B, 2000), u[-B:])
+    few, share = P.einet_choose(row.expand(5, 2000), tail)
+    assert torch.equal(index[-5:], few) and torch.equal(logq[-5:], share) and torch.equal(index[:5], few[:1].expand(5))
+    del u, index, logq
+    # scores of 1024 components: 64 lanes to a sample
+    N = 2 ** 26 + 5
+    print("route", N, flush=True)
+    score = torch.linspace(-3.0, 2.0, 1024, device="cuda")
+    ids, w, logp = P.einet_route(score[:, None].expand(1024, N), None, 1)
+    assert bool((ids == 1023).all()) and bool((w == w[0, 0]).all()) and bool((logp == logp[0]).all())
+    close(logp[-1:], [np.logaddexp.reduce(host(score))], U * 110)                  # (|logp| < 14)
+    del ids, w, logp
+    # rows: all samples are one row and few of them go anywhere
+    for name, H, n in (("a wave to a row", 256, 2 ** 26 + 5), ("a workgroup to a row", 300, 2 ** 24 + 5)):
+        print("rows,", name, n, flush=True)
+        place = torch.full((n, 1), -1, dtype=torch.int32, device="cuda")
+        went = torch.tensor([0, 1, 2 ** 24 - 5, 2 ** 24 - 4, 2 ** 24, n - 2, n - 1], device="cuda")
+        place[went, 0] = torch.arange(7, dtype=torch.int32, device="cuda")
+        x = torch.randn(1, H, device="cuda")
+        out = torch.zeros(8, H, device="cuda")
+        P.einet_dispatch(x.expand(n, H), place, out=out)
+        assert torch.equal(out[:7], x.expand(7, H)) and not bool(out[7].any())
+        weight = torch.full((n, 1), 2.0, device="cuda")
+        d, dw = P.einet_combine_backward(x.expand(n, H), out, place, weight)
+        assert torch.equal(d[:7], 2.0 * x.expand(7, H))
+        want = float(x.double().square().sum())
+        assert bool(((dw[went, 0].double() - want).abs() <= U * (H / 64 + 82) * want).all())
+        assert int(dw.count_nonzero()) == 7

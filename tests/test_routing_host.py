@@ -158,3 +158,13 @@ def test_binding_takes_no_tensors_of_the_host():
                  lambda: P.einet_combine_backward(x, x, place, torch.ones(4, 1)), lambda: P.einet_choose(x, torch.zeros(4))):
         with pytest.raises(AssertionError):
             call()
+
+
+def test_rows_too_long_for_a_launch_are_refused():
+    lib = P.load_library()
+    for width in ((1 << 35) + 1, 1 << 62):
+        _refused(lib.einet_dispatch(X, width, 0, 4, 2, X, X, width, 8, None), "einet_dispatch", "2^35")
+    for dtype, most in ((0, 1 << 33), (1, 1 << 34), (2, 1 << 34)):
+        for width in (most + 1, 1 << 61):
+            _refused(lib.einet_combine(X, dtype, width, 0, 8, X, X, 4, 2, X, width, None), "einet_combine", "2^35")
+            _refused(lib.einet_combine_backward(X, 0, X, dtype, width, 0, 8, X, X, 4, 2, X, width, X, None), "2^35")
