@@ -462,7 +462,8 @@ __global__ __launch_bounds__(256) void k_route_backward_columns(const T* __restr
 }
 
 // dcoef[c] = sum of the rows of `partial`, in float64: a workgroup has 32 columns and 32 interleaved shares of the rows
-__global__ __launch_bounds__(1024) void k_route_coef(const float* __restrict__ partial, int rows, int M, float* __restrict__ dcoef) {
+__global__ __launch_bounds__(1024) void k_route_coef(const float* __restrict__ partial, int rows, int M,
+                                                    float* __restrict__ dcoef) {
     __shared__ double sums[32][33];
     const int x = threadIdx.x & 31, share = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
     double v = 0.0;

@@ -78,8 +78,9 @@ class Mixture:
         """One pass of hard EM: every sample goes to one component, which runs einet_em_epoch on its samples in their order.
         The component is the most probable one, or with u (float32 [N] uniforms) drawn from the posterior, or given by ids
         (int32 [N]; -1: the sample is left out, as is one that no component has a density for).  The coefficients move by
-        `step` towards the posteriors' means over the samples before the pass (Eq. 7-9 with the mixture's own E-step).  Returns ids and, per sample, the log-density under its component at
-        the time it was visited (0 for those left out).  batch, em: as in einet_em_epoch."""
+        `step` towards the posteriors' means over the samples before the pass (Eq. 7-9 with the mixture's own E-step).  Returns
+        ids and, per sample, the log-density under its component at the time it was visited (0 for those left out).  batch, em:
+        as in einet_em_epoch."""
         N = x.shape[0]
         logp = self._torch.zeros(N, dtype=self._torch.float32, device=self.device)
         if N == 0:
@@ -89,7 +90,11 @@ class Mixture:
             if u is None:
                 ids = einet_route(rows, self.log_coef, 1)[0].view(N)
             else:
-                ids = einet_choose((rows + self.log_coef[:, None]).t().contiguous(), u)[0]
+                # (log-densities are in the thousands: the differences that matter, taken first, are exact in float32, while
+                # a sum with the coefficients would round them away)
+                largest = rows.amax(0)
+                rest = rows - self._torch.where(largest.isfinite(), largest, 0.0)
+                ids = einet_choose((rest + self.log_coef[:, None]).t().contiguous(), u)[0]
         place, segments = self._segments(ids.view(N, 1))
         counts = einet_route_backward(rows, self.log_coef, None, None, None, self._torch.ones_like(logp))[1]
         mine = einet_dispatch(x, place)

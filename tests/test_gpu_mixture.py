@@ -169,3 +169,26 @@ def test_training_command_reassigns_samples():
     r = subprocess.run([sys.executable, "-m", "paper_2004_06231_amd.train", "--graphs", "--reassign", "best"], capture_output=True, text=True,
                        timeout=110, cwd=root)
     assert r.returncode != 0 and "--reassign" in r.stderr
+
+
+@pytest.mark.parametrize("size", [0.0, -2.0 ** 20, 2.0 ** 20])
+def test_components_are_drawn_with_their_coefficients_whatever_the_size_of_the_densities(size):
+    """Densities that are equal leave the draw to the coefficients: 0.52 and 0.48, whose logarithms next to 2^20 would be rounded
+    to eighths (0.53 and 0.47).  Samples that no component, or one, has a finite density for too."""
+    _, models = components(2, 32)
+
+    class Given(P.Mixture):
+        def component_logp(self, x, mask=None):
+            return rows
+
+    x = dev(data(6))
+    rows = torch.full((2, 6), size, device="cuda")
+    rows[:, 3] = -math.inf
+    rows[0, 4] = -math.inf
+    rows[1, 5] = math.inf
+    u = torch.tensor([0.515, 0.525, 0.0, 0.5, 0.0, 0.0], device="cuda")
+    mix = Given(models, torch.tensor([0.52, 0.48]).log())
+    ids, _ = mix.em_epoch(x, batch=16, u=u, **EM)
+    assert ids.tolist() == [0, 1, 0, -1, 1, 1]
+    for m in models:
+        m.close()
