@@ -419,7 +419,9 @@ int einet_choose_workspace(int n_rows, int n_entries, size_t* bytes);
  *   min_p   of those the entries with at least min_p times the largest weight (0: all)
  * The choice is the first index, ascending, whose running sum of kept weights exceeds u times their total: what
  * einet_sample does with weights, here from their logarithms.  temperature 0: the first entry of the order, whatever
- * the filters.  Weights are summed as whole multiples of 2^-(61 - ceil(log2 n_entries)) of the largest, exactly.
+ * the filters.  Weights are summed exactly as whole multiples of a unit: up to 2^19 entries 2^-(61 - ceil(log2 n_entries)) of the
+ * largest, so that rounding changes a total by at most 2^-24 of the largest; in longer rows a unit of the row's own, at most
+ * 1.5 * 2^-60 of the total of its weights, so that rounding changes the total of those kept by at most 2^-29 of itself.
  *   logit_dev   device, [n_rows][n_entries] of `dtype`, rows row_stride elements apart (0: the same row for all)
  *   u_dev       device, [n_rows] float32 in [0,1) (below 0 or NaN counts as 0, from 1 on as the last kept entry)
  *   temperature_dev, top_k_dev, top_p_dev, min_p_dev   device, [n_rows] settings of every row, or NULL: then the value

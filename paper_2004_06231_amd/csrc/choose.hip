@@ -8,6 +8,12 @@
 // that their sums are exact and the same in whatever order they are formed, by atomics too.  A weight is off by half a unit
 // at most, 2^-61 of V times the largest; sums of float64 lose more where V is below 2^10, and no sum of float32 could tell
 // the entries of a long row apart: a uniform falls between two of V running sums.
+//
+// The total of V weights is off by V^2 2^-62 of the largest: less than float32 resolves (2^-24) up to V = 2^19, but a quarter at
+// 2^30, where every weight below 2^-32 would be lost.  Rows of more than FIXED_UNIT entries therefore get the unit that
+// their own total allows: a launch before the others sums the weights in the coarse units above, which bounds the total by Z, and
+// shift = 61 - ceil(log2 Z) then holds all of them: V weights are off by V 2^-60 of their total, 2^-30 at 2^30 entries.  (Kept ones
+// of the total that is kept: n of them are off by n 2^-60 Z, and Z is at most their total and V times the least of them.)
 #include "device_common.hpp"
 #include "routing.hpp"
 
@@ -16,6 +22,8 @@ namespace einet_impl {
 namespace {
 
 typedef unsigned long long u64;
+
+constexpr int FIXED_UNIT = 1 << 19;                              // entries up to which one unit does for every row
 
 // ------------------------------------------------------------------------------------------------ keys and weights
 
@@ -718,6 +726,7 @@ __global__ __launch_bounds__(NT, 4) void k_choose_block(ChooseArgs a, int shift)
 // Long rows: `parts` workgroups of SPLIT_THREADS for every row, each with a stretch of `per` entries, in four launches (three
 // where no filter is on) for every batch of SPLIT_ROWS rows.
 //   max      the largest order key of every part
+//   scale    the weights of every part summed in coarse units, for rows of more than FIXED_UNIT entries
 //   bins     the row's histogram over the distance from the largest logit, summed up by integer atomics (exact, in any
 //            order); rows without top_k and top_p: the kept mass of every part instead
 //   collect  the bin that the cut lies in, from the row's histogram.  With top_k: all entries up to that bin go to a list,
@@ -737,6 +746,7 @@ struct SplitRows {
     int parts, per;              // per: a multiple of 4 * SPLIT_THREADS
     u64* best;                   // [B][parts]
     uint32_t* low;               // [B][parts] complements of the lowest keys
+    u64* coarse;                 // [B][parts] sums of the weights in coarse units, or nullptr (up to FIXED_UNIT entries)
     u64* mass;                   // [B][parts][STRETCHES] kept masses
     u64* bin_mass;               // [B][SPLIT_BINS]
     uint32_t* bin_count;         // [B][SPLIT_BINS]
@@ -754,13 +764,19 @@ struct SplitRow {
     bool done;                   // no entry, or the largest one
     RowWeights<T> weight;
     float per_bin;
-    __device__ __forceinline__ SplitRow(const ChooseArgs& a, const SplitRows& sp, int row, int shift) {
+    // shift: of the units that the row's length allows; where the row has units of its own they replace it once `scaled`
+    __device__ __forceinline__ SplitRow(const ChooseArgs& a, const SplitRows& sp, int row, int shift, bool scaled = true) {
         st = row_settings(a, row);
         const int lane = threadIdx.x & 63;
         best = wave_reduce(lane < sp.parts ? sp.best[(size_t)row * sp.parts + lane] : 0, OpMax{});
         const uint32_t low = wave_reduce(lane < sp.parts ? sp.low[(size_t)row * sp.parts + lane] : 0u, OpMax{});
         const uint32_t kmax = (uint32_t)(best >> 32);
         done = kmax == 0u || st.greedy;
+        if (scaled && sp.coarse && !done) {
+            // every weight is at most half a coarse unit above what it counts for: total <= (sum + V / 2) units, and one more
+            const u64 sum = wave_reduce(lane < sp.parts ? sp.coarse[(size_t)row * sp.parts + lane] : 0, OpAdd{});
+            shift += __clzll(sum + a.V / 2) - 3;                 // 61 - ceil(log2(sum + V / 2 + 1))
+        }
         weight = RowWeights<T>{kmax, key_logit<T>(kmax), st.log2e_t, shift};
         per_bin = bins_per_unit(weight.m, key_logit<T>(~low), st.inv_t, SPLIT_BINS);
     }
@@ -800,6 +816,20 @@ __global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_max(ChooseArgs a
 __device__ __forceinline__ void write_stretch(const SplitRows& sp, int row, int part, u64 sum) {
     sum = wave_reduce(sum, OpAdd{});
     if ((threadIdx.x & 63) == 0) sp.mass[((size_t)row * sp.parts + part) * STRETCHES + (threadIdx.x >> 6)] = sum;
+}
+
+template <class T>
+__global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_scale(ChooseArgs a, SplitRows sp, int shift) {
+    __shared__ u64 tmp[SPLIT_THREADS / 64];
+    const int row = blockIdx.x / sp.parts, part = blockIdx.x - row * sp.parts;
+    const SplitRow<T> r(a, sp, row, shift, false);
+    if (r.done) return;
+    RowLogits<T, SPLIT_THREADS, 0> keys;
+    split_part(a, sp, row, part, keys);
+    u64 sum = 0;
+    keys.each([&](int, float v) { sum += r.weight(v); });
+    sum = block_reduce<SPLIT_THREADS>(sum, tmp, OpAdd{});
+    if (threadIdx.x == 0) sp.coarse[(size_t)row * sp.parts + part] = sum;
 }
 
 template <class T>
@@ -914,7 +944,7 @@ __global__ __launch_bounds__(FINISH_THREADS) void k_choose_split_finish(ChooseAr
     const bool by_count = r.by_count(a.V), by_mass = r.by_mass();
     const uint32_t listed = by_count || by_mass ? sp.listed[row] : 0;
     if (listed > LIST || (by_count && r.st.top_k > LIST)) {
-        choose_block<T, FINISH_THREADS, 0>(a, row, shift, sh);
+        choose_block<T, FINISH_THREADS, 0>(a, row, r.weight.shift, sh);
         return;
     }
     for (uint32_t i = tid; i < listed; i += FINISH_THREADS) list[i] = sp.list[(size_t)row * LIST + i];
@@ -1015,6 +1045,8 @@ size_t split_layout(int B, int V, char* p, SplitRows& sp) {
     };
     take(sp.best, (size_t)B * sp.parts);
     take(sp.low, (size_t)B * sp.parts);
+    if (V > FIXED_UNIT) take(sp.coarse, (size_t)B * sp.parts);
+    else sp.coarse = nullptr;
     take(sp.mass, (size_t)B * sp.parts * STRETCHES);
     take(sp.bin_mass, (size_t)B * SPLIT_BINS);
     take(sp.bin_count, (size_t)B * SPLIT_BINS);
@@ -1043,6 +1075,7 @@ void launch_choose_split(const ChooseArgs& a, const SplitRows& sp, int shift, hi
     const dim3 parts(a.B * sp.parts), rows(a.B);
     hipLaunchKernelGGL(k_choose_split_max<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp);
     const bool weighted = a.temperature.p || a.temperature.v > 0.f;          // (else the largest entry it is)
+    if (weighted && sp.coarse) hipLaunchKernelGGL(k_choose_split_scale<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp, shift);
     if (weighted) hipLaunchKernelGGL(k_choose_split_bins<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp, shift);
     const bool filters = a.top_k.p || a.top_p.p || (a.top_k.v > 0 && a.top_k.v < a.V) || a.top_p.v < 1.f;
     if (weighted && filters) hipLaunchKernelGGL(k_choose_split_collect<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp, shift);

@@ -643,3 +643,96 @@ def test_more_rows_than_a_launch_has_lanes_for():
         want = float(x.double().square().sum())
         assert bool(((dw[went, 0].double() - want).abs() <= U * (H / 64 + 82) * want).all())
         assert int(dw.count_nonzero()) == 7
+
+
+# ------------------------------------------------------------------------------------------------ choose, very long rows
+#
+# A row of more than 2^19 entries holds its weights as whole multiples of at most 1.5 * 2^-60 of their total Z (of the largest:
+# 1): a weight is off by half of that, V of them by V 2^-60 of the total at most, so a log-share by U |logq| + 2^-36 + V 2^-60 (up to 2^19
+# entries by V 2^-43, as above).  Among entries of weight W a running sum that is off by V 2^-60 Z is off by V 2^-60 Z / W entries, twice
+# (the sum and the total), and by one where a quotient is rounded down.
+
+def longest_tolerance(V, logq):
+    return U * np.abs(logq) + 2.0 ** -36 + V * (2.0 ** -60 if V > 1 << 19 else 2.0 ** -43)
+
+
+@pytest.mark.parametrize("V,dtype", [((1 << 19) + 1, "float32"), ((1 << 20) + 3, "float16"), ((1 << 23) + 1, "bfloat16"), ((1 << 26) + 5, "float32"),
+                                     (1 << 30, "bfloat16")])
+def test_choose_keeps_the_mass_of_many_small_weights(V, dtype):
+    """One entry at 0, all others so far below it that each is less than half of 2^-(61 - ceil(log2 V)), together up to a fifth of
+    the mass: their shares, and which of them a uniform falls on."""
+    print("choose among many small weights", V, dtype, flush=True)
+    level = -math.ceil((62 - (V - 1).bit_length()) * math.log(2.0) * 4 + 0.2) / 4       # (a multiple of 1/4 below 32: exact in every type)
+    W, big = math.exp(level), V // 3
+    Z = 1.0 + (V - 1) * W
+    row = torch.full((1, V), level, device="cuda", dtype=TYPES[dtype])
+    row[0, big] = 0.0
+    u = np.array([0.0, 2.0 ** -27, 2.0 ** -25, 0.3, 0.5, 0.999, 1.0 - 2.0 ** -24], np.float32)
+    index, logq = P.einet_choose(row.expand(len(u), V), torch.tensor(u).cuda())
+    slack = 2 * V * 2.0 ** -60 * Z / W + 2
+    for i, q, t in zip(host(index).tolist(), host(logq).tolist(), u.astype(np.float64) * Z):
+        want = int(t / W) if t < big * W else big if t < big * W + 1.0 else big + 1 + int((t - big * W - 1.0) / W)
+        assert 0 <= i < V and abs(i - want) <= (0 if want == big and i == big else slack), (i, want, slack)
+        share = (0.0 if i == big else level) - math.log(Z)
+        assert abs(q - share) <= longest_tolerance(V, share), (i, q, share)
+    if V > 1 << 21:
+        return
+    # the cut of top_p among them (entries of one weight are kept from the lowest index on): the last kept entry
+    p = float(np.float32(1.0 - 2.0 ** -24))
+    kept = math.ceil((p * Z - 1.0) / W)
+    index, _ = P.einet_choose(row, torch.ones(1, device="cuda"), top_p=p)
+    want = kept - 1 if kept <= big else kept
+    assert abs(int(index) - want) <= slack, (int(index), want)
+
+
+@pytest.mark.parametrize("V", [(1 << 19), (1 << 19) + 1, (1 << 22) + 7])
+def test_choose_from_very_long_rows_matches_the_formula(V):
+    """Against sorted weights summed in 80-bit floats."""
+    rng = np.random.default_rng(V)
+    B = 3
+    x = rng.normal(0, 3, (B, V)).astype(np.float32)
+    x[1, rng.random(V) < 0.4] = -np.inf
+    x[2] = -30.0 - 0.001 * np.abs(x[2])
+    x[2, 12345] = 0.0
+    dev = torch.tensor(x).cuda()
+    u = uniforms(rng, B)
+    for settings in (dict(), dict(temperature=0.7, top_k=300), dict(top_p=0.95), dict(min_p=1e-3), dict(temperature=1.5, top_p=0.999, min_p=1e-7), dict(top_k=5000)):
+        print("choose", V, settings, flush=True)
+        index, logq = P.einet_choose(dev, u, **settings)
+        T, k, p, mp = (settings.get(n, d) for n, d in (("temperature", 1.0), ("top_k", 0), ("top_p", 1.0), ("min_p", 0.0)))
+        T, p, mp = (float(np.float32(v)) for v in (T, p, mp))
+        for b in range(B):
+            left = np.flatnonzero(x[b] > -np.inf)
+            left = left[np.argsort(-x[b][left], kind="stable")]
+            if k > 0:
+                left = left[:k]
+            top = np.longdouble(x[b][left[0]])
+            w = np.exp((x[b][left].astype(np.longdouble) - top) / np.longdouble(T))
+            if p < 1:
+                run = np.cumsum(w)
+                n = 1 + int(np.count_nonzero(run[:-1] < np.longdouble(p) * run[-1]))
+                left, w = left[:n], w[:n]
+            left, w = left[w >= mp], w[w >= mp]
+            back = np.argsort(left)
+            left, w = left[back], w[back]
+            run = np.cumsum(w)
+            at = int(np.searchsorted(run, np.longdouble(float(u[b])) * run[-1], side="right"))
+            assert int(index[b]) == left[at], (b, int(index[b]), int(left[at]))
+            share = float(np.log(w[at] / run[-1]))
+            assert abs(float(logq[b]) - share) <= longest_tolerance(V, share), (b, float(logq[b]), share)
+
+
+def test_choose_from_very_long_rows_that_are_flat_empty_or_infinite():
+    V = (1 << 19) + 3
+    x = torch.zeros(5, V, device="cuda")
+    x[1] = -math.inf
+    x[2, 1::3] = math.inf
+    x[3] = torch.finfo(torch.float32).min
+    x[4, 77] = 1.0
+    u = torch.tensor([0.75, 0.5, 0.5, 0.25, 0.5], device="cuda")
+    t = torch.tensor([1.0, 1.0, 2.0, 0.5, 0.0], device="cuda")
+    index, logq = P.einet_choose(x, u, temperature=t)
+    n = (V + 1) // 3                                 # entries at 1, 4, 7, ...
+    assert host(index).tolist() == [int(0.75 * V), -1, 1 + 3 * (n // 2), int(0.25 * V), 77]
+    want = np.array([-math.log(V), -math.inf, -math.log(n), -math.log(V), 0.0])
+    close(logq, want, longest_tolerance(V, np.where(np.isfinite(want), want, 0.0)))
