@@ -90,11 +90,13 @@ class Mixture:
             if u is None:
                 ids = einet_route(rows, self.log_coef, 1)[0].view(N)
             else:
-                # (log-densities are in the thousands: the differences that matter, taken first, are exact in float32, while
-                # a sum with the coefficients would round them away)
-                largest = rows.amax(0)
-                rest = rows - self._torch.where(largest.isfinite(), largest, 0.0)
-                ids = einet_choose((rest + self.log_coef[:, None]).t().contiguous(), u)[0]
+                # (log-densities are in the thousands, where float32 would round the coefficients away: the sums, and their
+                # differences from the largest of the components that take part, are formed in float64 as einet_route does)
+                t = rows.double() + self.log_coef.double()[:, None]
+                t = self._torch.where(t.isnan(), -math.inf, t)
+                largest = t.amax(0)
+                rest = t - self._torch.where(largest.isfinite(), largest, 0.0)
+                ids = einet_choose(rest.float().t().contiguous(), u)[0]
         place, segments = self._segments(ids.view(N, 1))
         counts = einet_route_backward(rows, self.log_coef, None, None, None, self._torch.ones_like(logp))[1]
         mine = einet_dispatch(x, place)

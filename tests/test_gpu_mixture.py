@@ -192,3 +192,29 @@ def test_components_are_drawn_with_their_coefficients_whatever_the_size_of_the_d
     assert ids.tolist() == [0, 1, 0, -1, 1, 1]
     for m in models:
         m.close()
+
+
+def test_components_are_drawn_with_their_coefficients_next_to_closed_ones_and_without_a_number():
+    """A component that takes no part (its coefficient -inf, or its density NaN) has no say in how the others are drawn, however much
+    larger its density is."""
+    _, models = components(3, 32)
+
+    class Given(P.Mixture):
+        def component_logp(self, x, mask=None):
+            return rows
+
+    x = dev(data(8))
+    u = torch.tensor([0.515, 0.525, 0.515, 0.525, 0.0, 0.99, 0.3, 0.3], device="cuda")
+    for size in (-2.0 ** 20, 2.0 ** 20):
+        rows = torch.full((3, 8), size, device="cuda")
+        rows[2] = size + 2.0 ** 21
+        rows[2, 2:4] = math.nan
+        rows[2, 4] = math.inf                        # (closed: +inf and -inf make no number)
+        rows[0, 4:6] = math.nan
+        rows[:, 6] = math.nan
+        rows[:2, 7] = -math.inf
+        mix = Given(models, torch.tensor([0.52, 0.48, 0.0]).log())
+        ids, _ = mix.em_epoch(x, batch=16, u=u, **EM)
+        assert ids.tolist() == [0, 1, 0, 1, 1, 1, -1, -1]
+    for m in models:
+        m.close()
