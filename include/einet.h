@@ -136,8 +136,10 @@ int einet_create(const einet_spec* spec, einet_t** out);
 /* Frees the handle and its host tables.  Never touches caller buffers. */
 void einet_destroy(einet_t* h);
 
-/* Reason of the last error on this handle (or of the last failed
- * einet_create when h is NULL).  Host string owned by the library. */
+/* Reason of the last error on this handle, or, when h is NULL, of the last
+ * failed call without a handle (einet_create among them) of the calling
+ * thread: such calls may be made in several threads at once.  Host string
+ * owned by the library, valid until the next failure of its kind. */
 const char* einet_last_error(const einet_t* h);
 
 /* Sizes the caller must allocate on the device: n_params and n_stats in

@@ -59,7 +59,7 @@ struct einet {
 
 namespace {
 
-std::string g_create_error;
+thread_local std::string g_error;      // of calls without a handle, which several threads may make at once
 
 size_t append(std::vector<int32_t>& blob, const std::vector<int32_t>& v) {
     while (blob.size() % 64) blob.push_back(0);   // 256-byte alignment of every table
@@ -73,7 +73,7 @@ size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 int fail(const einet_t* h, int code, const std::string& msg) {
     if (h) h->err = msg;
-    else g_create_error = msg;
+    else g_error = msg;
     return code;
 }
 
@@ -296,7 +296,7 @@ void einet_destroy(einet_t* h) {
     delete h;
 }
 
-const char* einet_last_error(const einet_t* h) { return h ? h->err.c_str() : g_create_error.c_str(); }
+const char* einet_last_error(const einet_t* h) { return h ? h->err.c_str() : g_error.c_str(); }
 
 int einet_sizes(const einet_t* h, size_t* n_params, size_t* n_stats, size_t* workspace_bytes) {
     if (!h) return EINET_ERR_INVALID_ARG;

@@ -168,3 +168,32 @@ def test_rows_too_long_for_a_launch_are_refused():
         for width in (most + 1, 1 << 61):
             _refused(lib.einet_combine(X, dtype, width, 0, 8, X, X, 4, 2, X, width, None), "einet_combine", "2^35")
             _refused(lib.einet_combine_backward(X, 0, X, dtype, width, 0, 8, X, X, 4, 2, X, width, X, None), "2^35")
+
+
+def test_every_thread_reads_the_reason_of_its_own_refusal():
+    """Calls without a handle may be refused in several threads at once: nobody reads another call's reason."""
+    import threading
+    lib = P.load_library()
+    calls = [(lambda: lib.einet_route(X, 9, 8, 1, None, 4, 8, 2, 0, X, X, X, None), b"einet_route: unknown dtype"),
+             (lambda: lib.einet_choose(X, 0, 8, -1, 8, X, None, 1.0, None, 0, None, 1.0, None, 0.0, X, X, X, 0, None),
+              b"einet_choose: n_rows must be at least 0 and n_entries in 1..EINET_CHOOSE_MAX_ENTRIES"),
+             (lambda: lib.einet_sort(X, 8, 0, X, X, X, 0, None), b"einet_sort: n_components must be in 1..EINET_ROUTE_MAX_COMPONENTS"),
+             (lambda: lib.einet_dispatch(X, 64, 64, 4, 0, X, X, 64, 8, None), b"einet_dispatch: top must be at least 1")]
+    wrong = []
+    start = threading.Barrier(len(calls))
+
+    def refused(call, reason):
+        start.wait()
+        for _ in range(20000):
+            call()
+            got = lib.einet_last_error(None)
+            if got != reason:
+                wrong.append((reason, got))
+                return
+
+    threads = [threading.Thread(target=refused, args=c) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong
