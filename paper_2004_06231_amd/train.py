@@ -10,8 +10,8 @@ the first epoch and replayed from then on, which takes the host's launch calls o
 the clusters of the synthetic data hold for the first epoch only: before every later one all samples are routed
 anew, each to its most probable component (best) or to one drawn from its posterior (draw), and the coefficients
 follow.  Prints one JSON line: training throughput over all epochs and over the epochs after the first (which also loads the
-kernels), seconds per epoch, mean training logP of each epoch (first component) and the mean mixture logP of
-a held-out batch.
+kernels), seconds per epoch, mean training logP of each epoch (first component; null where no sample was routed to
+it) and the mean mixture logP of a held-out batch.
 
     python -m paper_2004_06231_amd.train --shape svhn --components 8 --epochs 3 --n 5000 --streams 4 --graphs
     python -m paper_2004_06231_amd.train --shape svhn --components 8 --epochs 5 --n 5000 --streams 4 --reassign best
@@ -108,7 +108,8 @@ def main():
         torch.cuda.synchronize()
         seconds.append(round(time.perf_counter() - t1, 4))
         first = lps[0] if mixture is None or e == 0 else lp[ids == 0]
-        history.append(round(float(first.mean()), 3))
+        # (no samples may be left to the first component: that is null in the line, which knows no NaN)
+        history.append(round(float(first.mean()), 3) if first.numel() else None)
         if args.graphs and e == 0 and args.epochs > 1:
             capture()                                    # (its time counts in the total, not in an epoch's)
     dt = time.perf_counter() - t0

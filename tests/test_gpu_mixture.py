@@ -218,3 +218,24 @@ def test_components_are_drawn_with_their_coefficients_next_to_closed_ones_and_wi
         assert ids.tolist() == [0, 1, 0, 1, 1, 1, -1, -1]
     for m in models:
         m.close()
+
+
+def test_training_command_with_a_component_that_keeps_no_samples(monkeypatch, capsys):
+    """All samples go to the second component: the line stays valid JSON, the first component's mean is null."""
+    from paper_2004_06231_amd import train
+    epoch = P.Mixture.em_epoch
+
+    def to_the_second(self, x, mask=None, **args):
+        return epoch(self, x, mask, **dict(args, u=None, ids=torch.ones(x.shape[0], dtype=torch.int32, device="cuda")))
+
+    monkeypatch.setattr(P.Mixture, "em_epoch", to_the_second)
+    monkeypatch.setattr(sys, "argv", "train --components 2 --n 600 --epochs 2 --streams 2 --reassign best".split())
+    train.main()
+    line = capsys.readouterr().out.strip().splitlines()[-1]
+
+    def refuse(name):
+        raise AssertionError(f"{name} in {line}")
+
+    out = json.loads(line, parse_constant=refuse)
+    history = out["train_mean_logp_per_epoch_component0"]
+    assert math.isfinite(history[0]) and history[1] is None and math.isfinite(out["held_out_mixture_mean_logp"])
