@@ -15,7 +15,8 @@ from .binding import (einet_choose, einet_combine, einet_dispatch, einet_mixture
 
 class Mixture:
     """components: bound EiNet models over the same variables; log_coef: float32 [n_components] or None for equal ones.
-    streams: torch streams that the components' work is spread over (the current stream alone by default)."""
+    streams: torch streams that the components' work is spread over (the current stream alone by default); a model that is
+    several components has all its work on one of them."""
 
     def __init__(self, components, log_coef=None, streams=None):
         import torch
@@ -28,6 +29,8 @@ class Mixture:
         if log_coef is not None:
             self.log_coef.copy_(self._torch.as_tensor(log_coef))
         self.streams = list(streams or [])
+        # (a model's workspace holds one call at a time: its calls follow each other on one stream)
+        self._first_of_model = [next(i for i, o in enumerate(self.components) if o is m) for m in self.components]
 
     @contextlib.contextmanager
     def _beside_each_other(self):
@@ -40,7 +43,7 @@ class Mixture:
         for s in self.streams:
             s.wait_stream(here)
         try:
-            yield lambda c: self._torch.cuda.stream(self.streams[c % len(self.streams)])
+            yield lambda c: self._torch.cuda.stream(self.streams[self._first_of_model[c] % len(self.streams)])
         finally:
             for s in self.streams:
                 here.wait_stream(s)

@@ -239,3 +239,25 @@ def test_training_command_with_a_component_that_keeps_no_samples(monkeypatch, ca
     out = json.loads(line, parse_constant=refuse)
     history = out["train_mean_logp_per_epoch_component0"]
     assert math.isfinite(history[0]) and history[1] is None and math.isfinite(out["held_out_mixture_mean_logp"])
+
+
+def test_a_model_that_is_several_components_works_on_one_stream():
+    """The calls on one model share its workspace: side by side on two streams they would overwrite each other's activations."""
+    _, (a, b) = components(2, 32)
+    _, (a2, b2) = components(2, 32)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    x = dev(data(150))
+    mix, plain = P.Mixture([a, b, a, b, a], streams=streams), P.Mixture([a2, b2, a2, b2, a2])
+    with mix._beside_each_other() as at:
+        used = []
+        for c in range(5):
+            with at(c):
+                used.append(torch.cuda.current_stream())
+    assert used == [streams[0], streams[1], streams[0], streams[1], streams[0]]
+    assert torch.equal(mix.component_logp(x), plain.component_logp(x))
+    ids = torch.arange(150, dtype=torch.int32, device="cuda") % 5
+    got, want = mix.em_epoch(x, batch=16, ids=ids, **EM)[1], plain.em_epoch(x, batch=16, ids=ids, **EM)[1]
+    assert torch.equal(got, want) and torch.equal(a.params, a2.params) and torch.equal(b.params, b2.params)
+    assert torch.equal(mix.log_coef, plain.log_coef)
+    for m in (a, b, a2, b2):
+        m.close()
