@@ -483,9 +483,16 @@ def _workspace(name, device, *sizes):
     return (torch.empty(n, dtype=torch.uint8, device=device) if n else None), n
 
 
+def _int32(n):
+    """A number that C takes as an int: one beyond is refused here, where ctypes would cut it."""
+    assert -2 ** 31 <= n < 2 ** 31, f"{n} is beyond 32 bits"
+    return n
+
+
 def _scores(scores, log_coef):
     import torch
     assert scores.is_cuda and scores.dim() == 2, "scores must be a cuda tensor [n_components, n]"
+    _int32(scores.shape[0])
     if log_coef is not None:
         _on(scores.device, torch.float32, scores.shape[:1], log_coef)
     return (scores.data_ptr(), _row_type(scores), scores.stride(0), scores.stride(1), _ptr(log_coef)) + tuple(scores.shape)
@@ -500,7 +507,7 @@ def einet_route(scores, log_coef=None, top=1, renormalise=False):
     import torch
     args = _scores(scores, log_coef)
     n, device = scores.shape[1], scores.device
-    ids = torch.empty(n, top, dtype=torch.int32, device=device)
+    ids = torch.empty(n, _int32(top), dtype=torch.int32, device=device)
     weights = torch.empty(n, top, dtype=torch.float32, device=device)
     logp = torch.empty(n, dtype=torch.float32, device=device)
     _enqueue("einet_route", device, *args, top, 1 if renormalise else 0, ids.data_ptr(), weights.data_ptr(), logp.data_ptr())
@@ -515,7 +522,7 @@ def einet_route_backward(scores, log_coef, ids, weights, dweights=None, dlogp=No
     args = _scores(scores, log_coef)
     (M, n), device = scores.shape, scores.device
     assert dweights is None or (ids is not None and weights is not None), "dweights needs ids and weights"
-    top = 1 if ids is None else ids.shape[1]
+    top = 1 if ids is None else _int32(ids.shape[1])
     _on(device, torch.int32, (n, top), ids)
     _on(device, torch.float32, (n, top), weights, dweights)
     _on(device, torch.float32, (n,), dlogp)
@@ -535,7 +542,7 @@ def einet_sort(ids, n_components):
     assert ids.is_cuda
     _on(ids.device, torch.int32, ids.shape, ids)
     place = torch.empty_like(ids)
-    first = torch.empty(n_components + 1, dtype=torch.int32, device=ids.device)
+    first = torch.empty(_int32(n_components) + 1, dtype=torch.int32, device=ids.device)
     ws, n_bytes = _workspace("einet_sort_workspace", ids.device, ids.numel(), n_components)
     _enqueue("einet_sort", ids.device, ids.data_ptr(), ids.numel(), n_components, first.data_ptr(), place.data_ptr(), _ptr(ws),
              n_bytes)
@@ -560,7 +567,7 @@ def _slots(place, n, device):
     import torch
     assert place.dim() == 2 and place.shape[0] == n, "place must have a row for every sample"
     _on(device, torch.int32, place.shape, place)
-    return place.shape[1]
+    return _int32(place.shape[1])
 
 
 def einet_dispatch(x, place, out=None):
@@ -631,10 +638,14 @@ def einet_choose(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     import torch
     assert logits.is_cuda and logits.dim() == 2
     n, V = logits.shape
+    _int32(n)
+    _int32(V)
     device = logits.device
     assert V <= 1 or logits.stride(1) == 1, "every row of logits must be contiguous"
     _on(device, torch.float32, (n,), u)
     settings = []
+    if isinstance(top_k, int):
+        top_k = max(-1, min(top_k, 2 ** 31 - 1))     # (more than any row has: all; ctypes would cut it to 32 bits)
     for v, dtype in ((temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32), (min_p, torch.float32)):
         if isinstance(v, (int, float)):
             settings += (None, v)

@@ -736,3 +736,27 @@ def test_choose_from_very_long_rows_that_are_flat_empty_or_infinite():
     assert host(index).tolist() == [int(0.75 * V), -1, 1 + 3 * (n // 2), int(0.25 * V), 77]
     want = np.array([-math.log(V), -math.inf, -math.log(n), -math.log(V), 0.0])
     close(logq, want, longest_tolerance(V, np.where(np.isfinite(want), want, 0.0)))
+
+
+def test_numbers_beyond_32_bits_are_not_cut():
+    """C takes numbers of components, entries and choices as ints: one beyond is refused, and a top_k beyond keeps all."""
+    dev = dict(device="cuda")
+    column = torch.zeros(1, 3, **dev)
+    with pytest.raises(AssertionError, match="32 bits"):
+        P.einet_route(column.expand(2 ** 32 + 2, 3))
+    with pytest.raises(AssertionError, match="32 bits"):
+        P.einet_route(torch.zeros(4, 0, **dev), top=2 ** 32 + 1)
+    with pytest.raises(AssertionError, match="32 bits"):
+        P.einet_sort(torch.zeros(0, 1, dtype=torch.int32, **dev), 2 ** 32 + 1)
+    with pytest.raises(AssertionError, match="32 bits"):
+        P.einet_choose(torch.zeros(0, 2 ** 32 + 5, **dev), torch.zeros(0, **dev))
+    with pytest.raises(AssertionError, match="32 bits"):
+        P.einet_dispatch(torch.zeros(0, 2, **dev), torch.zeros(0, 2 ** 32 + 1, dtype=torch.int32, **dev))
+    rng = np.random.default_rng(1)
+    x, u = torch.tensor(rng.normal(0, 1, (50, 7)).astype(np.float32)).cuda(), uniforms(rng, 50)
+    want = P.einet_choose(x, u)
+    for k in (7, 2 ** 31 - 1, 2 ** 31, 2 ** 32 + 1, 2 ** 63 - 1):
+        assert all(torch.equal(a, b) for a, b in zip(P.einet_choose(x, u, top_k=k), want))
+    for k in (-1, -2 ** 32, -2 ** 63):
+        with pytest.raises(P.EinetError):
+            P.einet_choose(x, u, top_k=k)
