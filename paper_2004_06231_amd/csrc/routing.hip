@@ -247,6 +247,9 @@ __global__ __launch_bounds__(256) void k_route_columns(const T* __restrict__ p, 
     logp[n] = dead ? -INFINITY : (float)((double)m + (double)logf(z));
 }
 
+// Sums of the gradients of the coefficients, a row for every wave of the workgroup.
+template <int G, int E, bool STAGED> constexpr size_t route_sums_bytes = sizeof(float) * (ROUTE_THREADS<G, STAGED> / 64) * G * E;
+
 // With a = sum_s dw[s] w[s]:
 //   d t[c] = p[c] (dlogp - a) + sum_{s: id[s] = c} dw[s] w[s]            (weights p)
 //   d t[c] = p[c] dlogp + sum_{s: id[s] = c} w[s] (dw[s] - a)            (weights that sum to one)
@@ -340,8 +343,9 @@ __global__ __launch_bounds__((ROUTE_THREADS<G, STAGED>)) void k_route_backward(c
         for (int e = 0; e < E; ++e) acc[e] += d[e];
     }
     if (!partial) return;
-    constexpr int WAVES = (NT + 63) / 64;
+    constexpr int WAVES = NT / 64;
     __shared__ float sums[WAVES][G * E];
+    static_assert(sizeof(sums) == route_sums_bytes<G, E, STAGED>, "what the launch allows for");
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         float v = acc[e];
@@ -501,6 +505,12 @@ bool route_by_columns(const Scores& a, int top) {
 }
 bool route_staged(const Scores& a) { return a.sn == 1 && a.sc != 1 && a.M > 16 && a.N >= 32 * EINET_NUM_CUS; }
 template <int G> size_t route_tile_bytes(int M) { return sizeof(float) * ROUTE_STAGE<G> * (size_t)(M | 1); }
+// Dynamic LDS of a workgroup that has `own` bytes besides: beyond 64 KiB in all the kernel has to be allowed it (the scores of
+// 512 components, their gradient for 257 to 512 and for 1024).
+template <class Kernel>
+void allow_tile(Kernel kernel, size_t tile, size_t own) {
+    if (tile + own > 65536) allow_dynamic_lds(kernel, tile);
+}
 
 // Workgroups of the gradient, which is the rows of its workspace.  A handful of samples are one workgroup's, whose sums are
 // the gradient of the coefficients: no second launch and no workspace.  Two to a compute unit, four where many samples are read
@@ -864,6 +874,7 @@ void launch_route(const Scores& a, int top, bool renormalise, int32_t* ids, floa
             auto go = [&](auto staged) {
                 constexpr bool STAGED = decltype(staged)::value;
                 constexpr int NT = ROUTE_THREADS<G, STAGED>, S = NT / G;
+                if constexpr (STAGED) allow_tile(k_route<T, K, G, E, STAGED>, route_tile_bytes<G>(a.M), 0);
                 row_batches(a.N, G, [&](int64_t n0, int64_t n) {
                     hipLaunchKernelGGL((k_route<T, K, G, E, STAGED>), dim3((unsigned)((n + S - 1) / S)), dim3(NT),
                                        STAGED ? route_tile_bytes<G>(a.M) : 0, s, p + n0 * a.sn, a.sc, a.sn, a.coef, a.M, n, top, re,
@@ -904,6 +915,8 @@ void launch_route_backward(const Scores& a, int top, bool renormalise, const int
                 constexpr int G = decltype(g)::value, E = decltype(e)::value;
                 auto go = [&](auto staged) {
                     constexpr bool STAGED = decltype(staged)::value;
+                    if constexpr (STAGED)
+                        allow_tile(k_route_backward<T, K, G, E, STAGED>, route_tile_bytes<G>(a.M), route_sums_bytes<G, E, STAGED>);
                     hipLaunchKernelGGL((k_route_backward<T, K, G, E, STAGED>), dim3(groups), dim3(ROUTE_THREADS<G, STAGED>),
                                        STAGED ? route_tile_bytes<G>(a.M) : 0, s, p, a.sc, a.sn, a.coef, a.M, a.N, top, re, ids, weights,
                                        dweights, dlogp, d, dsc, dsn, partial);

@@ -760,3 +760,39 @@ def test_numbers_beyond_32_bits_are_not_cut():
     for k in (-1, -2 ** 32, -2 ** 63):
         with pytest.raises(P.EinetError):
             P.einet_choose(x, u, top_k=k)
+
+
+@pytest.mark.parametrize("M", [257, 512, 1024])
+def test_captured_route_and_sort_of_many_components(M):
+    """Kernels whose workgroups have more than 64 KiB of LDS (scores of 512 components through LDS, their gradient for 257 to 512 and
+    1024, the sort of 1024), captured and replayed with eager work between."""
+    print("captured", M, flush=True)
+    N = 8200
+
+    def all_of(scores, coef, dw, dl):
+        ids, w, logp = P.einet_route(scores, coef, 2)
+        ds, da = P.einet_route_backward(scores, coef, ids, w, dw, dl)
+        return (ids, w, logp, ds, da) + P.einet_sort(ids, M)
+
+    def fresh(seed):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+        return [torch.randn(*s, generator=g, device="cuda") for s in ((M, N), (M,), (N, 2), (N,))]
+
+    state = fresh(0)
+    all_of(*state)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = all_of(*state)
+    for rep in range(3):
+        for t, v in zip(state, fresh(rep + 1)):
+            t.copy_(v)
+        g.replay()
+        torch.cuda.synchronize()
+        want = all_of(*state)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), f"replay {rep}"
+    t = state[0].double() + state[1].double()[:, None]
+    assert torch.equal(out[0][:, 0].long(), t.argmax(0))
+    close(out[2], host(t.logsumexp(0)), U * (host(t.logsumexp(0).abs()) + 96))
