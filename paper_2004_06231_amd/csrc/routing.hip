@@ -486,7 +486,7 @@ __global__ __launch_bounds__(1024) void k_route_coef(const float* __restrict__ p
 
 // Lanes per sample: as many as selections at least, and at most 16 components to a lane.
 int route_lanes(int M, int top) {
-    const int most = M <= 32 ? 4 : M <= 64 ? 4 : M <= 128 ? 8 : 16;   // components to a lane
+    const int most = M <= 64 ? 4 : M <= 128 ? 8 : 16;                 // components to a lane
     int G = 4;
     while (G < 64 && (G < top || G * most < M)) G *= 2;
     return G;
@@ -504,6 +504,7 @@ bool route_by_columns(const Scores& a, int top) {
     return a.sn == 1 && a.M <= ROUTE_COLUMNS_MOST && top <= 4 && a.N >= (a.M <= 16 ? 256 : 512) * EINET_NUM_CUS;
 }
 bool route_staged(const Scores& a) { return a.sn == 1 && a.sc != 1 && a.M > 16 && a.N >= 32 * EINET_NUM_CUS; }
+template <int G> constexpr bool ROUTE_CAN_STAGE = G > 4;               // (four lanes have up to 16 components)
 template <int G> size_t route_tile_bytes(int M) { return sizeof(float) * ROUTE_STAGE<G> * (size_t)(M | 1); }
 // Dynamic LDS of a workgroup that has `own` bytes besides: beyond 64 KiB in all the kernel has to be allowed it (the scores of
 // 512 components, their gradient for 257 to 512 and for 1024).
@@ -881,8 +882,9 @@ void launch_route(const Scores& a, int top, bool renormalise, int32_t* ids, floa
                                        ids + n0 * top, weights + n0 * top, logp + n0);
                 });
             };
-            if (route_staged(a)) go(std::true_type{});
-            else go(std::false_type{});
+            if constexpr (ROUTE_CAN_STAGE<G>)
+                if (route_staged(a)) return go(std::true_type{});
+            go(std::false_type{});
         });
     });
 }
@@ -921,8 +923,9 @@ void launch_route_backward(const Scores& a, int top, bool renormalise, const int
                                        STAGED ? route_tile_bytes<G>(a.M) : 0, s, p, a.sc, a.sn, a.coef, a.M, a.N, top, re, ids, weights,
                                        dweights, dlogp, d, dsc, dsn, partial);
                 };
-                if (staged_rows) go(std::true_type{});
-                else go(std::false_type{});
+                if constexpr (ROUTE_CAN_STAGE<G>)
+                    if (staged_rows) return go(std::true_type{});
+                go(std::false_type{});
             });
         });
     if (dcoef && (groups > 1 || a.N == 0))
