@@ -796,3 +796,26 @@ def test_captured_route_and_sort_of_many_components(M):
     t = state[0].double() + state[1].double()[:, None]
     assert torch.equal(out[0][:, 0].long(), t.argmax(0))
     close(out[2], host(t.logsumexp(0)), U * (host(t.logsumexp(0).abs()) + 96))
+
+
+def test_combine_of_more_rows_than_a_launch_has_lanes_for():
+    """Sums of more rows than one launch of 2^32 lanes has a wave for (64 lanes to 264 float16): rows on both sides of the border
+    between the launches, with weights and without, and zeros everywhere else."""
+    H, n = 264, 2 ** 26 + 5
+    border = (2 ** 32 - 1024) // 64
+    print("combine", H, n, flush=True)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    rows = torch.randn(9, H, generator=g, device="cuda").half()
+    place = torch.full((n, 1), -1, dtype=torch.int32, device="cuda")
+    went = torch.tensor([0, 1, border - 2, border - 1, border, border + 1, n - 3, n - 2, n - 1], device="cuda")
+    place[went, 0] = torch.arange(9, dtype=torch.int32, device="cuda")
+    weight = torch.zeros(n, 1, device="cuda")
+    weight[went, 0] = 2.0
+    out = torch.full((n, H), 7.0, dtype=torch.float16, device="cuda")
+    for w in (weight, None):
+        P.einet_combine(rows, place, w, out=out)
+        assert torch.equal(out[went], rows * 2.0 if w is not None else rows)
+        step = 2 ** 22
+        assert sum(int(out[b:b + step].any(1).sum()) for b in range(0, n, step)) == 9
+        out.fill_(7.0)
