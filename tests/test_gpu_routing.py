@@ -819,3 +819,56 @@ def test_combine_of_more_rows_than_a_launch_has_lanes_for():
         step = 2 ** 22
         assert sum(int(out[b:b + step].any(1).sum()) for b in range(0, n, step)) == 9
         out.fill_(7.0)
+
+
+@pytest.mark.parametrize("V", [50, 1500, 6000, 20000, 600000])
+def test_choose_at_the_ends_of_the_temperatures(V):
+    """An infinite temperature makes all entries that take part equal (those at +inf, where there are any); the smallest one leaves
+    the largest alone."""
+    rng = np.random.default_rng(V)
+    x = rng.normal(0, 4, (3, V)).astype(np.float32)
+    x[1, ::2] = -np.inf
+    x[2, 5::7] = np.inf
+    u = np.array([0.6, 0.3, 0.7], np.float32)
+    dev, du = torch.tensor(x).cuda(), torch.tensor(u).cuda()
+    part = [np.flatnonzero(x[0] > -np.inf), np.flatnonzero(x[1] > -np.inf), np.flatnonzero(x[2] == np.inf)]
+    for t in (math.inf, torch.full((3,), math.inf, device="cuda")):
+        for k in (0, 4):
+            print("choose, infinite temperature", V, k, flush=True)
+            index, logq = P.einet_choose(dev, du, temperature=t, top_k=k)
+            # (of equal weights the first top_k of the order: by logit, then by index)
+            kept = [np.sort(p[np.argsort(-x[b][p], kind="stable")][:k]) if k else p for b, p in enumerate(part)]
+            assert host(index).tolist() == [int(p[int(float(u[b]) * len(p))]) for b, p in enumerate(kept)]
+            want = np.array([-math.log(len(p)) for p in kept])
+            close(logq, want, longest_tolerance(V, want) + V * 2.0 ** -(62 - (V - 1).bit_length()) * (V <= 1 << 19))
+    for t in (2.0 ** -149, torch.full((3,), 2.0 ** -149, device="cuda")):
+        for settings in (dict(), dict(top_k=4), dict(top_p=0.5)):
+            index, logq = P.einet_choose(dev[:2], du[:2], temperature=t if not torch.is_tensor(t) else t[:2], **settings)
+            assert host(index).tolist() == x[:2].argmax(1).tolist() and not bool(logq.any())
+
+
+@pytest.mark.parametrize("B,V", [(3, 3001), (3, 20000), (2, (1 << 19) + 5)])
+def test_captured_choices_replay_on_new_logits(B, V):
+    def fresh(seed):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+        return [torch.randn(B, V, generator=g, device="cuda") * 2, torch.rand(B, generator=g, device="cuda"),
+                torch.randint(1, 900, (B,), generator=g, device="cuda", dtype=torch.int32)]
+
+    def choices(x, u, k):
+        return P.einet_choose(x, u) + P.einet_choose(x, u, top_p=0.9) + P.einet_choose(x, u, temperature=0.7, top_k=k, min_p=1e-4)
+
+    state = fresh(0)
+    choices(*state)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = choices(*state)
+    for rep in range(3):
+        for t, v in zip(state, fresh(rep + 1)):
+            t.copy_(v)
+        g.replay()
+        torch.cuda.synchronize()
+        want = choices(*state)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), f"replay {rep}"
