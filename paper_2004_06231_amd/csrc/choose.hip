@@ -756,27 +756,27 @@ struct SplitRows {
 
 enum SplitMode { SPLIT_NONE, SPLIT_ALL, SPLIT_COUNT, SPLIT_MASS, SPLIT_BLOCK };
 
-// What a row's workgroups agree on from its settings and the largest keys of its parts.
-template <class T>
+// What a row's workgroups agree on from its settings and the largest keys of its parts.  OWN: the row has units of its own.
+template <class T, bool OWN>
 struct SplitRow {
     RowSettings st;
     u64 best;
     bool done;                   // no entry, or the largest one
     RowWeights<T> weight;
     float per_bin;
-    // shift: of the units that the row's length allows; where the row has units of its own they replace it once `scaled`
-    __device__ __forceinline__ SplitRow(const ChooseArgs& a, const SplitRows& sp, int row, int shift, bool scaled = true) {
+    __device__ __forceinline__ SplitRow(const ChooseArgs& a, const SplitRows& sp, int row, int shift) {
         st = row_settings(a, row);
         const int lane = threadIdx.x & 63;
         best = wave_reduce(lane < sp.parts ? sp.best[(size_t)row * sp.parts + lane] : 0, OpMax{});
         const uint32_t low = wave_reduce(lane < sp.parts ? sp.low[(size_t)row * sp.parts + lane] : 0u, OpMax{});
         const uint32_t kmax = (uint32_t)(best >> 32);
         done = kmax == 0u || st.greedy;
-        if (scaled && sp.coarse && !done) {
-            // every weight is at most half a coarse unit above what it counts for: total <= (sum + V / 2) units, and one more
-            const u64 sum = wave_reduce(lane < sp.parts ? sp.coarse[(size_t)row * sp.parts + lane] : 0, OpAdd{});
-            shift += __clzll(sum + a.V / 2) - 3;                 // 61 - ceil(log2(sum + V / 2 + 1))
-        }
+        if constexpr (OWN)
+            if (!done) {
+                // every weight is at most half a coarse unit above what it counts for: total <= (sum + V / 2) units, and one more
+                const u64 sum = wave_reduce(lane < sp.parts ? sp.coarse[(size_t)row * sp.parts + lane] : 0, OpAdd{});
+                shift += __clzll(sum + a.V / 2) - 3;             // 61 - ceil(log2(sum + V / 2 + 1))
+            }
         weight = RowWeights<T>{kmax, key_logit<T>(kmax), st.log2e_t, shift};
         per_bin = bins_per_unit(weight.m, key_logit<T>(~low), st.inv_t, SPLIT_BINS);
     }
@@ -822,7 +822,7 @@ template <class T>
 __global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_scale(ChooseArgs a, SplitRows sp, int shift) {
     __shared__ u64 tmp[SPLIT_THREADS / 64];
     const int row = blockIdx.x / sp.parts, part = blockIdx.x - row * sp.parts;
-    const SplitRow<T> r(a, sp, row, shift, false);
+    const SplitRow<T, false> r(a, sp, row, shift);               // (the units that the row's length allows)
     if (r.done) return;
     RowLogits<T, SPLIT_THREADS, 0> keys;
     split_part(a, sp, row, part, keys);
@@ -832,12 +832,12 @@ __global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_scale(ChooseArgs
     if (threadIdx.x == 0) sp.coarse[(size_t)row * sp.parts + part] = sum;
 }
 
-template <class T>
+template <class T, bool OWN>
 __global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_bins(ChooseArgs a, SplitRows sp, int shift) {
     __shared__ u64 mass[SPLIT_BINS];
     __shared__ uint32_t count[SPLIT_BINS];
     const int row = blockIdx.x / sp.parts, part = blockIdx.x - row * sp.parts, tid = threadIdx.x;
-    const SplitRow<T> r(a, sp, row, shift);
+    const SplitRow<T, OWN> r(a, sp, row, shift);
     if (r.done) return;
     RowLogits<T, SPLIT_THREADS, 0> keys;
     split_part(a, sp, row, part, keys);
@@ -869,8 +869,8 @@ __global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_bins(ChooseArgs 
 }
 
 // The row's mode and the bin that its cut lies in; missing: what is to be reached within that bin (top_p alone).
-template <class T>
-__device__ __forceinline__ SplitMode split_cut_bin(const ChooseArgs& a, const SplitRows& sp, const SplitRow<T>& r, int row,
+template <class T, bool OWN>
+__device__ __forceinline__ SplitMode split_cut_bin(const ChooseArgs& a, const SplitRows& sp, const SplitRow<T, OWN>& r, int row,
                                                    ChooseShared<SPLIT_THREADS>& sh, int& bin, u64& missing) {
     const int tid = threadIdx.x, b = 2 * tid;
     if (r.done) return SPLIT_NONE;
@@ -891,14 +891,14 @@ __device__ __forceinline__ SplitMode split_cut_bin(const ChooseArgs& a, const Sp
     return SPLIT_MASS;
 }
 
-template <class T>
+template <class T, bool OWN>
 __global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_collect(ChooseArgs a, SplitRows sp, int shift) {
     __shared__ ChooseShared<SPLIT_THREADS> sh;
     __shared__ u64 mine[PART_LIST];                              // the part's entries of the list, in any order
     __shared__ uint32_t n_mine, base;
     const int row = blockIdx.x / sp.parts, part = blockIdx.x - row * sp.parts, tid = threadIdx.x;
     if (tid == 0) n_mine = 0;                                    // (read behind the barriers of split_cut_bin)
-    const SplitRow<T> r(a, sp, row, shift);
+    const SplitRow<T, OWN> r(a, sp, row, shift);
     int bin;
     u64 missing;
     const SplitMode mode = split_cut_bin(a, sp, r, row, sh, bin, missing);
@@ -931,12 +931,12 @@ __global__ __launch_bounds__(SPLIT_THREADS) void k_choose_split_collect(ChooseAr
     if (mode == SPLIT_MASS) write_stretch(sp, row, part, sum);
 }
 
-template <class T>
+template <class T, bool OWN>
 __global__ __launch_bounds__(FINISH_THREADS) void k_choose_split_finish(ChooseArgs a, SplitRows sp, int shift) {
     __shared__ ChooseShared<FINISH_THREADS> sh;
     __shared__ u64 list[LIST], stretch[SPLIT_PARTS * STRETCHES];
     const int row = blockIdx.x, tid = threadIdx.x;
-    const SplitRow<T> r(a, sp, row, shift);
+    const SplitRow<T, OWN> r(a, sp, row, shift);
     if (r.done) {
         if (tid == 0) write_choice(a, row, r.weight.kmax ? (int)~(uint32_t)r.best : -1, r.weight.kmax ? 0.f : -INFINITY);
         return;
@@ -1070,16 +1070,16 @@ ChooseArgs rows_from(const ChooseArgs& a, int b0, int n) {
     return r;
 }
 
-template <class T>
+template <class T, bool OWN>
 void launch_choose_split(const ChooseArgs& a, const SplitRows& sp, int shift, hipStream_t s) {
     const dim3 parts(a.B * sp.parts), rows(a.B);
     hipLaunchKernelGGL(k_choose_split_max<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp);
     const bool weighted = a.temperature.p || a.temperature.v > 0.f;          // (else the largest entry it is)
-    if (weighted && sp.coarse) hipLaunchKernelGGL(k_choose_split_scale<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp, shift);
-    if (weighted) hipLaunchKernelGGL(k_choose_split_bins<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp, shift);
+    if (OWN && weighted) hipLaunchKernelGGL(k_choose_split_scale<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp, shift);
+    if (weighted) hipLaunchKernelGGL((k_choose_split_bins<T, OWN>), parts, dim3(SPLIT_THREADS), 0, s, a, sp, shift);
     const bool filters = a.top_k.p || a.top_p.p || (a.top_k.v > 0 && a.top_k.v < a.V) || a.top_p.v < 1.f;
-    if (weighted && filters) hipLaunchKernelGGL(k_choose_split_collect<T>, parts, dim3(SPLIT_THREADS), 0, s, a, sp, shift);
-    hipLaunchKernelGGL(k_choose_split_finish<T>, rows, dim3(FINISH_THREADS), 0, s, a, sp, shift);
+    if (weighted && filters) hipLaunchKernelGGL((k_choose_split_collect<T, OWN>), parts, dim3(SPLIT_THREADS), 0, s, a, sp, shift);
+    hipLaunchKernelGGL((k_choose_split_finish<T, OWN>), rows, dim3(FINISH_THREADS), 0, s, a, sp, shift);
 }
 
 template <class T>
@@ -1101,8 +1101,11 @@ void launch_choose_rows(const ChooseArgs& a, int shift, hipStream_t s) {
     else if (V <= 4096) go(k_choose_block<T, 512, 2>, 512, 1);
     else if (split_layout(a.B, V, static_cast<char*>(a.workspace), sp) == 0) go(k_choose_block<T, 1024, 2>, 1024, 1);
     else
-        for (int64_t b0 = 0; b0 < a.B; b0 += SPLIT_ROWS)
-            launch_choose_split<T>(rows_from(a, (int)b0, min(a.B - (int)b0, SPLIT_ROWS)), sp, shift, s);
+        for (int64_t b0 = 0; b0 < a.B; b0 += SPLIT_ROWS) {
+            const ChooseArgs rows = rows_from(a, (int)b0, min(a.B - (int)b0, SPLIT_ROWS));
+            if (V > FIXED_UNIT) launch_choose_split<T, true>(rows, sp, shift, s);
+            else launch_choose_split<T, false>(rows, sp, shift, s);
+        }
 }
 
 }  // namespace
