@@ -148,7 +148,8 @@ class Mixture:
 
     def inpaint(self, x, mask, u, noise=None, top=1):
         """[N, D, C]: the observed variables (mask 1; uint8 [D] or [N, D]) as they are, the others as the `top` most probable
-        components given the observed ones complete them, weighted by their shares of the posterior.  u: float32
+        components given the observed ones complete them, weighted by their shares of the posterior (zeros where no component has a
+        density for the observed ones).  u: float32
         [choices(), N * top], noise: float32 [N * top, D, C] or None for leaf means, both as in einet_sample, in the order of
         the slots sorted by component."""
         ids, weights, _ = self.route(x, mask, top)

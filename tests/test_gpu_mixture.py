@@ -261,3 +261,21 @@ def test_a_model_that_is_several_components_works_on_one_stream():
     assert torch.equal(mix.log_coef, plain.log_coef)
     for m in (a, b, a2, b2):
         m.close()
+
+
+def test_inpainting_without_a_component_leaves_zeros():
+    _, models = components(2, 32)
+
+    class Given(P.Mixture):
+        def component_logp(self, x, mask=None):
+            return rows
+
+    x, mask = dev(data(5)), dev(masks(np.random.default_rng(4), 5, "per_sample"))
+    rows = torch.zeros(2, 5, device="cuda")
+    rows[:, 3] = -math.inf
+    mix = Given(models)
+    got = mix.inpaint(x, mask, torch.rand(mix.choices(), 10, device="cuda"), top=2)
+    seen = mask.bool()[:, :, None]
+    assert torch.equal(got[seen], x[seen]) and not bool(got[3][~seen[3]].any()) and bool(got[2][~seen[2]].any())
+    for m in models:
+        m.close()
