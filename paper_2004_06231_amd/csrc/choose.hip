@@ -204,7 +204,7 @@ __device__ __forceinline__ V wave_reduce(V v, Op op) { return lane_value(wave_sc
 //
 // Rows of up to 1024 entries stay in the registers of one wave: group g, lane l, place c is entry (g * 64 + l) * VEC + c.
 // A cut is found by halving the range of keys: the entries above the middle are counted by ballots, their weights summed
-// over the lanes.  The vector ALU bounds it: 50176 rows of 256 (51 MB) take 31 us without filters, 47 with top-k, 61 with
+// over the lanes.  The vector ALU bounds it: 50176 rows of 256 (51 MB) take 30 us without filters, 46 with top-k, 63 with
 // top-p, some 700 instructions for a row, of which the float64 exponentials are 120 and a halving 28.  (A workgroup with bins for
 // every row: 8192 rows of 500 45 us instead of 10, with top-p 90 instead of 21.)
 template <class T, int VEC, int GROUPS>
@@ -389,8 +389,8 @@ __global__ __launch_bounds__(256) void k_choose_wave(ChooseArgs a, int shift) {
 //
 // A cut is found from the histogram of the entries over their distance from the largest logit in units of T (BINS equal bins
 // to 32 units; their order is the entries' order): the bin that the cut lies in holds few entries of an ordinary row, and a
-// radix search over the order keys of that bin's entries finds the very entry.  One row of 4000 takes 7 us without filters and
-// 16 with all, most of it the latency of the some twenty steps between barriers; 4096 rows of 2048 (34 MB) 32 and 73 us.
+// radix search over the order keys of that bin's entries finds the very entry.  One row of 4000 takes 6 us without filters and
+// 16 with all, most of it the latency of the some twenty steps between barriers; 4096 rows of 2048 (34 MB) 33 and 77 us.
 template <class T, int NT, int GROUPS>
 struct RowLogits {
     const T* x;
@@ -723,8 +723,8 @@ __global__ __launch_bounds__(NT, 4) void k_choose_block(ChooseArgs a, int shift)
 
 // ------------------------------------------------------------------------------------ several workgroups for every row
 //
-// Long rows: `parts` workgroups of SPLIT_THREADS for every row, each with a stretch of `per` entries, in four launches (three
-// where no filter is on) for every batch of SPLIT_ROWS rows.
+// Long rows: `parts` workgroups of SPLIT_THREADS for every row, each with a stretch of `per` entries, in four launches (one
+// less where no filter is on, one more for units of the row's own) for every batch of SPLIT_ROWS rows.
 //   max      the largest order key of every part
 //   scale    the weights of every part summed in coarse units, for rows of more than FIXED_UNIT entries
 //   bins     the row's histogram over the distance from the largest logit, summed up by integer atomics (exact, in any
@@ -733,11 +733,12 @@ __global__ __launch_bounds__(NT, 4) void k_choose_block(ChooseArgs a, int shift)
 //            at most LIST of them.  With top_p alone: that bin's entries do, and every part's kept mass in the bins before it
 //            is written down.
 //   finish   one workgroup per row finds the cut among the list's entries, the choice among them (top_k) or in the part in
-//            which the running sum exceeds the target.  A row whose list did not hold its entries (more than LIST entries, or
-//            PART_LIST of one part, nearly as large as each other) and one with top_k above LIST are done as a workgroup for
-//            every row does it.
-// One row of 131077 takes 13 us without filters and 23 with all, all of it launches and their latency; 64 rows (34 MB) 33 and
-// 40 us (largest keys 9, bins 10, list 15, finish 9).
+//            which the running sum exceeds the target.  A row whose list did not hold its entries (more than LIST in all or
+//            PART_LIST of one part: nearly equal ones, or a large top_k of few parts, from some 1500 on of two) and one with
+//            top_k above LIST are done as a workgroup for every row does it: right, but slow.
+// One row of 131077 takes 14 us without filters and 25 with all, all of it launches and their latency; 64 rows (34 MB) 34 us (9
+// largest keys, 16 masses, 10 finish) and 43 us (9 largest keys, 9 bins, 14 list, 11 finish); one row of 2^20 35 and 47 us, of which
+// its own units cost 9 us.
 constexpr int SPLIT_THREADS = 256, SPLIT_BINS = 2 * SPLIT_THREADS, LIST = 4096, PART_LIST = 1024, FINISH_THREADS = 256;
 constexpr int SPLIT_PARTS = 64;                                  // at most (a lane each)
 constexpr int STRETCHES = SPLIT_THREADS / 64;                    // of a part: its waves'
@@ -1023,7 +1024,8 @@ __global__ __launch_bounds__(FINISH_THREADS) void k_choose_split_finish(ChooseAr
 
 // Parts of a row, 0 for rows that a workgroup does alone: up to 4096 entries, and up to 8192 (it keeps their logits in its
 // registers) as long as all rows run at once, two to a compute unit.  Measured with all filters, us, alone and split: 64 rows
-// of 8000 26 and 29, 1000 of 8000 95 and 51, 300 of 25000 101 and 39, 500 of 16384 75 and 38.
+// of 8000 26 and 29, 1000 of 8000 95 and 51, 300 of 25000 101 and 39, 500 of 16384 75 and 38.  A part has some 4096 entries
+// of few rows, and as many more as fewer workgroups than that make of many rows (two for each beyond 512) or long ones.
 constexpr int SPLIT_WORKGROUPS = 1024, SPLIT_ROWS = 1024;        // in a batch of rows; rows of a batch
 int split_parts(int B, int V) {
     if (V <= 4096 || (V <= 8192 && B <= 2 * EINET_NUM_CUS)) return 0;

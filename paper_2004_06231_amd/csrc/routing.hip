@@ -184,8 +184,8 @@ void k_route(const T* __restrict__ p, int64_t sc, int64_t sn, const float* __res
 
 // A sample to a lane, for components whose samples are next to each other: the loads of a component are contiguous over
 // the lanes, and up to MOST components of a sample are in registers.  262144 samples of 64 components: 17 us with one
-// selection and no coefficients (4.1 TB/s), 25 us with two and coefficients, whose float64 sums the vector ALU does in 55 %
-// of the time.
+// selection and no coefficients (4.1 TB/s), 24 us with two and coefficients: the loads of all components come first, then two
+// float64 sums of each, so neither memory (2.9 TB/s) nor the vector ALU (busy 57 % of the time) is full.
 constexpr int ROUTE_COLUMNS_MOST = 64;
 template <class T, class K, int TOP, int MOST>
 __global__ __launch_bounds__(256) void k_route_columns(const T* __restrict__ p, int64_t sc, const float* __restrict__ coef, int M,
@@ -365,7 +365,7 @@ __global__ __launch_bounds__((ROUTE_THREADS<G, STAGED>)) void k_route_backward(c
 // The same with a sample to a lane and up to MOST components in registers.  The gradients of a component are summed over the
 // lanes by folding: a step adds two halves of the lanes and keeps of every pair of components one in each half, so that 64
 // components take 63 additions, not 64 times 6, and lane l is left with the sum of component l (16: with that of l % 16).
-// 262144 samples of 64 components: 45 us, 3.0 TB/s read and written.
+// 262144 samples of 64 components: 45 to 47 us, 3.0 TB/s read and written.
 template <int CTRL>
 __device__ __forceinline__ float fold(float a, float b, bool second) {
     return (second ? b : a) + lane_of<CTRL>(second ? a : b);
@@ -484,7 +484,15 @@ __global__ __launch_bounds__(1024) void k_route_coef(const float* __restrict__ p
     }
 }
 
-// Lanes per sample: as many as selections at least, and at most 16 components to a lane.
+// Lanes per sample: as many as selections at least, and at most 16 components to a lane.  Measured with rows of float32 scores
+// and coefficients, four selections, us without / with gradient, by components to a lane,
+//                  16000 samples                                       500 samples
+//   components     2           4           8           16              2          4          8          16
+//   32             4.1 / 7.1   3.8 / 6.6   4.1 / 7.6   4.0 / 7.9       3.1 / 5.7  3.3 / 6.1  3.7 / 6.9  3.7 / 7.1
+//   64             6.0 / 10.2  4.7 / 8.2   4.5 / 7.9   5.7 / 10.4      3.5 / 6.0  3.3 / 6.5  3.9 / 7.3  5.2 / 9.7
+//   128            10.1 / 16.2 7.2 / 11.7  6.0 / 10.2  6.5 / 11.3      3.8 / 6.3  3.8 / 6.9  4.0 / 7.4  5.5 / 9.7
+//   256            12.5 / 20.3 12.0 / 20.1 9.7 / 15.5  9.1 / 15.2      4.2 / 6.8  4.4 / 6.7  4.6 / 7.3  5.6 / 9.3
+// The rule is that of many samples; a few hundred of more than 64 components would do better with fewer to a lane.
 int route_lanes(int M, int top) {
     const int most = M <= 64 ? 4 : M <= 128 ? 8 : 16;                 // components to a lane
     int G = 4;
@@ -492,14 +500,24 @@ int route_lanes(int M, int top) {
     return G;
 }
 
-// Which kernel takes scores whose samples are next to each other (sn = 1).  Measured with log coefficients at 64 components,
-// two selections (16 components, one, without): us without and with gradient,
-//   samples                     8192         16384        65536         131072        262144
-//   groups of lanes, directly   4.7 / 8.2    6.4 / 11     15 / 34       29 / 63       51 / 117   (3.9 / 8.5 at 65536)
-//   groups of lanes, through LDS 4.6 / 8.2   5.5 / 9.3    11 / 22       23 / 40       43 / 72    (4.1 / 12.7)
-//   a lane per sample           12 / 23      12 / 23      12 / 26       16 / 31       25 / 48    (4.1 / 7.9)
+// Which kernel takes scores whose samples are next to each other (sn = 1).  Measured with log coefficients and two selections, us
+// without / with gradient (of weights and log-density),
+//   components                     samples: 8192       65536         131072         262144
+//   16     groups of lanes, directly      3.5 / 6.7    4.5 / 9.2     5.9 / 11.5     9.1 / 18.2
+//          a lane per sample              4.4 / 8.8    4.6 / 9.7     5.5 / 10.8     7.2 / 17.2
+//   24     groups of lanes, directly      3.4 / 6.5    6.1 / 11.6    9.2 / 16.0     15.7 / 30.6
+//          groups of lanes, through LDS   3.6 / 7.0    5.8 / 14.0    9.3 / 21.6     15.7 / 50.5
+//          a lane per sample              6.3 / 18.8   6.6 / 19.7    7.9 / 22.9     11.9 / 36.5
+//   64     groups of lanes, directly      4.2 / 8.0    14.5 / 28.1   27.5 / 53.4    49.4 / 93.4
+//          groups of lanes, through LDS   4.3 / 7.9    10.7 / 21.5   21.9 / 39.7    41.7 / 71.7
+//          a lane per sample              11.3 / 22.8  11.2 / 25.1   13.7 / 30.3    23.3 / 47.4
+//   256    groups of lanes, directly      9.5 / 17.9   52 / 101      98 / 203       200 / 546
+//          groups of lanes, through LDS   8.1 / 14.3   44 / 60       83 / 127       173 / 291
+//   1024   groups of lanes, directly      56 / 99      357 / 1067
+//          groups of lanes, through LDS   35 / 46      223 / 451
 // A lane per sample waits for one chain of loads and needs every compute unit full of waves; a wide row of few components
-// is read well enough directly.
+// is read well enough directly.  The rule is the same with gradient and without; of 17 to 32 components, whose lane per sample
+// goes through 64, the gradient alone would do better directly at any number of samples.
 bool route_by_columns(const Scores& a, int top) {
     return a.sn == 1 && a.M <= ROUTE_COLUMNS_MOST && top <= 4 && a.N >= (a.M <= 16 ? 256 : 512) * EINET_NUM_CUS;
 }
@@ -553,8 +571,11 @@ void with_type(int type, F&& f) {
 // -1 for a slot without a component.  Block b has the b-th stretch of the slots and wave w of it the w-th stretch of that.
 // A slot's position: the slots of lower components, those of its own in the blocks and waves before, and its rank among
 // those of the wave.  Few slots are one workgroup's; more are counted in a first launch, one row of counts per block.
-// Latency bounds both: 1024 slots of 128 components take 4.4 us, 32768 8.3 us (30 in one workgroup), a million 25 us.
-// One workgroup against two launches: 4096 slots 6.1 and 6.5 us, 6000 slots 7.5 and 6.9.
+// Latency bounds both: 1024 slots of 128 components take 4.4 us, 32768 8.3 us (30 in one workgroup), a million 25 us, where
+// the 64 workgroups do.
+// One workgroup against two launches: 4096 slots 6.1 and 6.5 us, 6000 slots 7.5 and 6.9.  At most 64, 128 and 256 workgroups (64
+// components): 131072 slots 9.8, 11.7 and 11.6 us, 262144 11.7, 12.7 and 17.4, a million 23, 19 and 21, four million 72, 48 and 36:
+// every workgroup reads the counts of all, which 64 keep short for up to some half a million slots.
 constexpr int SORT_WAVES = 16;
 constexpr int SORT_ONE_BLOCK = 4096, SORT_MOST_BLOCKS = 64;
 
